@@ -71,7 +71,10 @@ typedef enum {
 typedef enum {
     HS_F32 = 0,        /* IEEE binary32 */
     HS_BF16 = 1,       /* bfloat16 (upper half of binary32), stored as uint16 */
-    HS_FP8_E4M3 = 2    /* OCP fp8 E4M3 ("fn": bias 7, max 448, no inf), uint8 */
+    HS_FP8_E4M3 = 2,   /* OCP fp8 E4M3 ("fn": bias 7, max 448, no inf), uint8 */
+    HS_FP4_E2M1 = 3    /* OCP fp4 E2M1 (0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives),
+                          two codes a byte, the even column in the low half; packed
+                          row tables only (hs_row_table) */
 } hs_dtype;
 
 /* Shape of one merge window (one call sequence). */
@@ -392,6 +395,135 @@ hs_status hs_priority(const hs_plan *plan, const int32_t *inverse, const int32_t
                       const float *s_hat, const uint8_t *heavy, double alpha, double gamma,
                       double delta, double eps, double *phi_fused, double *pi, int32_t *order,
                       void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------- row tables
+ *
+ * Both ends of a language model work on a table of rows, one per token (or, in
+ * a retrieval window, one per chunk): token rows are looked up and their
+ * gradients summed, hidden rows are multiplied with the table (usually kept in
+ * four bits for serving), the resulting scores are adjusted and the best columns
+ * taken.  A row table in device memory, described on the host: */
+typedef struct {
+    const void *data;     /* [rows x dim] row-major; FP4: [rows x dim / 2] bytes.
+                             16-byte aligned */
+    const void *scale;    /* FP8: [rows] fp32, value = scale[r] * code;
+                             FP4: [rows x dim / group], value = scale[r][c / group] * code;
+                             else NULL */
+    int64_t rows;         /* 0 <= rows <= 2^31 - 1 */
+    int64_t dim;          /* 1 <= dim <= 16384; FP4: a multiple of group */
+    int32_t dtype;        /* HS_F32, HS_BF16, HS_FP8_E4M3 or HS_FP4_E2M1 */
+    int32_t scale_dtype;  /* FP4: HS_F32 or HS_BF16; else ignored */
+    int32_t group;        /* FP4: 32, 64 or 128 columns share a scale; else ignored */
+} hs_row_table;
+
+/* Packs rows into four bits: per group, scale = amax / 6 rounded to scale_dtype
+ * and code = src / scale (fp32 division) rounded to the nearest E2M1 value, ties
+ * to the even code, magnitudes above 6 to 6.  A group whose scale is 0 gets codes
+ * 0.  (A table with OCP MX block scales 2^e needs no packing: its scales are
+ * exact in bf16, with group = 32.)
+ *   src     [rows x dim] device, HS_F32 or HS_BF16, finite, 16-byte aligned
+ *   codes   [rows x dim / 2] bytes device out, 16-byte aligned
+ *   scale   [rows x dim / group] scale_dtype device out
+ * Bit-exact and deterministic. */
+hs_status hs_pack_rows(const void *src, int32_t src_dtype, int64_t rows, int64_t dim,
+                       int32_t group, int32_t scale_dtype, void *codes, void *scale,
+                       void *stream);
+
+/* Embedding lookup with scaling: out[i] = scale * T[ids[i]], i < n, decoded and
+ * scaled in fp32 and rounded once to out_dtype.  Ids outside [0, rows) and ids
+ * equal to pad_id (-1: no such id) stand for no token: their rows are zeros.
+ *   ids      [n] int32 (ids_is_i64 = 0) or int64 (= 1) device, 0 <= n <= 2^30
+ *   out      [n x dim] device out, HS_F32 or HS_BF16, aligned to its element
+ *            (16-byte rows use 128-bit accesses) */
+hs_status hs_embed(const hs_row_table *table, const void *ids, int32_t ids_is_i64, int64_t n,
+                   float scale, int64_t pad_id, void *out, int32_t out_dtype, void *stream);
+
+/* Gradient of hs_embed with respect to its table:
+ *   d_table[v] = scale * sum of d_out[i] over the i with ids[i] = v
+ * (accumulate = 1: added to d_table[v]), ids that stand for no token left out.  The
+ * positions are sorted by token (stable); each row is summed in fp32 in an order
+ * that depends on n and dim and the ids alone, scaled, and rounded once to
+ * d_table_dtype: deterministic.  Rows of tokens that do not occur become zeros
+ * (accumulate = 1: are left untouched).
+ *   d_out    [n x dim] device, HS_F32 or HS_BF16
+ *   d_table  [rows x dim] device, HS_F32 or HS_BF16: out (accumulate = 0) or in and
+ *            out (1).  Both aligned to their elements (16-byte aligned rows use
+ *            128-bit accesses)
+ *   ws       device, 256-byte aligned, of hs_embed_grad_bytes' size */
+hs_status hs_embed_grad_bytes(int64_t n, int64_t rows, int64_t dim, size_t *bytes);
+hs_status hs_embed_grad(const void *d_out, int32_t d_out_dtype, const void *ids,
+                        int32_t ids_is_i64, int64_t n, int64_t rows, int64_t dim, float scale,
+                        int64_t pad_id, int32_t accumulate, void *d_table,
+                        int32_t d_table_dtype, void *ws, size_t ws_bytes, void *stream);
+
+/* Products of a few rows with every row of a packed table (an output head for
+ * single tokens; the scores of few queries over a 4-bit corpus):
+ *   out[m][r] = sum over groups g of scale[r][g] * sum_{c in g} x[m][c] * code[r][c]
+ * Products are exact (fp32 x in three bf16 parts), sums in fp32, one rounding to
+ * out_dtype.  Equal table rows get bit-identical scores.
+ *   table      an HS_FP4_E2M1 table
+ *   x          [n_x x dim] device, HS_F32 or HS_BF16, 16-byte aligned; 0 <= n_x <= 2^20
+ *              (finite: a NaN or infinity in row m makes out[m] NaN)
+ *   out        [n_x x out_stride] device out, HS_F32 or HS_BF16, out_stride >= rows
+ *              elements; columns [rows, out_stride) are left as they were
+ * Tables are read once for up to 64 rows of x. */
+hs_status hs_score_packed(const hs_row_table *table, const void *x, int32_t x_dtype, int64_t n_x,
+                          void *out, int32_t out_dtype, int64_t out_stride, void *stream);
+
+/* Adjustments of rows of scores (logits), one row per sequence (or query).  Any
+ * of the lists and arrays may be NULL: that adjustment is left out. */
+typedef struct {
+    const int64_t *seen_off;     /* [n_rows + 1]: row r's tokens are seen[seen_off[r]
+                                    .. seen_off[r + 1]) */
+    const int32_t *seen;         /* [n_seen] repeated tokens: prompt, then output */
+    int64_t n_seen;
+    const int32_t *prompt_len;   /* [n_rows] the first prompt_len[r] entries are the
+                                    prompt (NULL: 0) */
+    const float *repetition;     /* [n_rows] > 0 */
+    const float *frequency;      /* [n_rows] */
+    const float *presence;       /* [n_rows] */
+    const int64_t *bias_off;     /* [n_rows + 1]: row r's biases are entries
+                                    bias_off[r] .. bias_off[r + 1] */
+    const int32_t *bias_id;      /* [n_bias] columns */
+    const float *bias;           /* [n_bias] */
+    int64_t n_bias;
+    const uint32_t *allow;       /* column c is allowed where bit c % 32 of word c / 32
+                                    is set */
+    int64_t allow_stride;        /* words from one row's mask to the next; 0: one mask
+                                    for all rows; else >= ceil(n_cols / 32) */
+} hs_adjust;
+
+/* For every row r < n_rows and column c < n_cols, in fp32 and rounded once:
+ *   x = scores[r][c]
+ *   c among the row's seen tokens:        x = x > 0 ? x / repetition[r] : x * repetition[r]
+ *   c seen n > 0 times after the prompt:  x = (x - frequency[r] * n) - presence[r]
+ *   c among the row's biases:             x = x + bias (the last entry of c)
+ *   c not allowed:                        x = -inf, whatever it was
+ * List entries outside [0, n_cols) are skipped; offsets are clamped to their
+ * list (a reversed range is empty).
+ *   scores/out  [n_rows x stride] device, HS_F32 or HS_BF16 both, aligned to their
+ *               elements, each with its own stride >= n_cols (elements; columns
+ *               from n_cols on are left as they were); out may be scores itself
+ *               (same stride), else the two must not overlap
+ * 0 <= n_rows <= 2^20, 0 <= n_cols <= 2^31 - 1; n_rows * n_cols <= 2^40. */
+hs_status hs_adjust_scores(const hs_adjust *adjust, const void *scores, int64_t stride, void *out,
+                           int64_t out_stride, int32_t dtype, int64_t n_rows, int64_t n_cols,
+                           void *stream);
+
+/* The k best columns of every row of scores: score descending, equal scores by
+ * ascending column (-0 as +0), as hs_score_topk orders rows of a corpus.  Entries
+ * of -inf (columns not allowed) and NaN are never taken; slots left are (-inf, -1).
+ *   scores      [n_rows x stride] device, HS_F32 or HS_BF16, aligned to its element,
+ *               stride >= n_cols elements; 0 <= n_rows <= 2^20, 0 <= n_cols <= 2^31 - 1
+ *   k           1 <= k <= 1024 (k > n_cols pads)
+ *   topk_score  [n_rows x k] fp32 device out
+ *   topk_index  [n_rows x k] int32 device out
+ *   ws          device, 256-byte aligned, of hs_topk_rows_bytes' size
+ * Bit-exact and deterministic. */
+hs_status hs_topk_rows_bytes(int64_t n_rows, int64_t n_cols, int32_t k, size_t *bytes);
+hs_status hs_topk_rows(const void *scores, int32_t dtype, int64_t stride, int64_t n_rows,
+                       int64_t n_cols, int32_t k, float *topk_score, int32_t *topk_index,
+                       void *ws, size_t ws_bytes, void *stream);
 
 const char *hs_status_string(hs_status s);
 const char *hs_last_error(void);

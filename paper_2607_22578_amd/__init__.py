@@ -32,15 +32,17 @@ _lib = ctypes.CDLL(LIB_PATH)
 
 HS_OK, HS_ERR_INVALID_ARG, HS_ERR_UNSUPPORTED, HS_ERR_WORKSPACE, HS_ERR_ALIGNMENT, \
     HS_ERR_DEVICE = range(6)
-HS_F32, HS_BF16, HS_FP8_E4M3 = 0, 1, 2
+HS_F32, HS_BF16, HS_FP8_E4M3, HS_FP4_E2M1 = 0, 1, 2, 3
 ABI_VERSION = 3
 
 EXPORTS = ["hs_merge_plan", "hs_plan_destroy", "hs_workflow_rows", "hs_dedup", "hs_score_topk",
            "hs_score_topk_noalloc", "hs_score_partial", "hs_topk_merge", "hs_corpus_tiled_bytes",
            "hs_tile_corpus", "hs_scatter", "hs_deliver",
            "hs_cache_bytes", "hs_cache_reset", "hs_cache_lookup",
-           "hs_cache_insert", "hs_signature", "hs_priority", "hs_status_string",
-           "hs_last_error", "hs_abi_version"]
+           "hs_cache_insert", "hs_signature", "hs_priority",
+           "hs_pack_rows", "hs_embed", "hs_embed_grad_bytes", "hs_embed_grad",
+           "hs_score_packed", "hs_adjust_scores", "hs_topk_rows_bytes", "hs_topk_rows",
+           "hs_status_string", "hs_last_error", "hs_abi_version"]
 HS_SIG_NORMALIZE_TEXT = 1
 HS_FLAG_TILED_CORPUS = 1
 
@@ -61,6 +63,22 @@ class hs_sig_nodes(ctypes.Structure):
                 ("text_bytes", ctypes.c_int64), ("pred_off", ctypes.c_void_p),
                 ("pred_idx", ctypes.c_void_p), ("pred_count", ctypes.c_int64),
                 ("n_nodes", ctypes.c_int64)]
+
+
+class hs_row_table(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("scale", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("dim", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("scale_dtype", ctypes.c_int32), ("group", ctypes.c_int32)]
+
+
+class hs_adjust(ctypes.Structure):
+    _fields_ = [("seen_off", ctypes.c_void_p), ("seen", ctypes.c_void_p),
+                ("n_seen", ctypes.c_int64), ("prompt_len", ctypes.c_void_p),
+                ("repetition", ctypes.c_void_p), ("frequency", ctypes.c_void_p),
+                ("presence", ctypes.c_void_p), ("bias_off", ctypes.c_void_p),
+                ("bias_id", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("n_bias", ctypes.c_int64), ("allow", ctypes.c_void_p),
+                ("allow_stride", ctypes.c_int64)]
 
 
 _vp, _i64, _i32, _sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t
@@ -103,6 +121,27 @@ _dbl = ctypes.c_double
 _lib.hs_priority.argtypes = ([_vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _dbl, _dbl, _dbl, _dbl]
                              + [_vp] * 4 + [_sz, _vp])
 _lib.hs_priority.restype = ctypes.c_int
+_flt = ctypes.c_float
+_lib.hs_pack_rows.argtypes = [_vp, _i32, _i64, _i64, _i32, _i32, _vp, _vp, _vp]
+_lib.hs_pack_rows.restype = ctypes.c_int
+_lib.hs_embed.argtypes = [ctypes.POINTER(hs_row_table), _vp, _i32, _i64, _flt, _i64, _vp, _i32,
+                          _vp]
+_lib.hs_embed.restype = ctypes.c_int
+_lib.hs_embed_grad_bytes.argtypes = [_i64, _i64, _i64, ctypes.POINTER(_sz)]
+_lib.hs_embed_grad_bytes.restype = ctypes.c_int
+_lib.hs_embed_grad.argtypes = [_vp, _i32, _vp, _i32, _i64, _i64, _i64, _flt, _i64, _i32, _vp, _i32,
+                               _vp, _sz, _vp]
+_lib.hs_embed_grad.restype = ctypes.c_int
+_lib.hs_score_packed.argtypes = [ctypes.POINTER(hs_row_table), _vp, _i32, _i64, _vp, _i32, _i64,
+                                 _vp]
+_lib.hs_score_packed.restype = ctypes.c_int
+_lib.hs_adjust_scores.argtypes = [ctypes.POINTER(hs_adjust), _vp, _i64, _vp, _i64, _i32, _i64,
+                                  _i64, _vp]
+_lib.hs_adjust_scores.restype = ctypes.c_int
+_lib.hs_topk_rows_bytes.argtypes = [_i64, _i64, _i32, ctypes.POINTER(_sz)]
+_lib.hs_topk_rows_bytes.restype = ctypes.c_int
+_lib.hs_topk_rows.argtypes = [_vp, _i32, _i64, _i64, _i64, _i32, _vp, _vp, _vp, _sz, _vp]
+_lib.hs_topk_rows.restype = ctypes.c_int
 _lib.hs_status_string.argtypes = [ctypes.c_int]
 _lib.hs_status_string.restype = ctypes.c_char_p
 _lib.hs_last_error.argtypes = []
@@ -334,6 +373,57 @@ def hs_priority(plan: Plan, inverse, first_index, n_unique: int, n_unique_dev, p
                             _ptr(n_unique_dev), _ptr(phi), _ptr(s_hat), _ptr(heavy), alpha, gamma,
                             delta, eps, _ptr(phi_fused), _ptr(pi), _ptr(order), _ptr(ws),
                             _ws_bytes(ws, ws_bytes), _stream(stream)))
+
+
+def hs_pack_rows(src, src_dtype: int, rows: int, dim: int, group: int, scale_dtype: int, codes,
+                 scale, stream=None):
+    _check(_lib.hs_pack_rows(_ptr(src), src_dtype, rows, dim, group, scale_dtype, _ptr(codes),
+                             _ptr(scale), _stream(stream)))
+
+
+def hs_embed(table: hs_row_table, ids, ids_is_i64: int, n: int, scale: float, pad_id: int, out,
+             out_dtype: int, stream=None):
+    _check(_lib.hs_embed(ctypes.byref(table), _ptr(ids), ids_is_i64, n, scale, pad_id, _ptr(out),
+                         out_dtype, _stream(stream)))
+
+
+def hs_embed_grad_bytes(n: int, rows: int, dim: int) -> int:
+    b = _sz()
+    _check(_lib.hs_embed_grad_bytes(n, rows, dim, ctypes.byref(b)))
+    return int(b.value)
+
+
+def hs_embed_grad(d_out, d_out_dtype: int, ids, ids_is_i64: int, n: int, rows: int, dim: int,
+                  scale: float, pad_id: int, accumulate: int, d_table, d_table_dtype: int,
+                  ws=None, ws_bytes: Optional[int] = None, stream=None):
+    _check(_lib.hs_embed_grad(_ptr(d_out), d_out_dtype, _ptr(ids), ids_is_i64, n, rows, dim, scale,
+                              pad_id, accumulate, _ptr(d_table), d_table_dtype, _ptr(ws),
+                              _ws_bytes(ws, ws_bytes), _stream(stream)))
+
+
+def hs_score_packed(table: hs_row_table, x, x_dtype: int, n_x: int, out, out_dtype: int,
+                    out_stride: int, stream=None):
+    _check(_lib.hs_score_packed(ctypes.byref(table), _ptr(x), x_dtype, n_x, _ptr(out), out_dtype,
+                                out_stride, _stream(stream)))
+
+
+def hs_adjust_scores(adjust: hs_adjust, scores, stride: int, out, out_stride: int, dtype: int,
+                     n_rows: int, n_cols: int, stream=None):
+    _check(_lib.hs_adjust_scores(ctypes.byref(adjust), _ptr(scores), stride, _ptr(out), out_stride,
+                                 dtype, n_rows, n_cols, _stream(stream)))
+
+
+def hs_topk_rows_bytes(n_rows: int, n_cols: int, k: int) -> int:
+    b = _sz()
+    _check(_lib.hs_topk_rows_bytes(n_rows, n_cols, k, ctypes.byref(b)))
+    return int(b.value)
+
+
+def hs_topk_rows(scores, dtype: int, stride: int, n_rows: int, n_cols: int, k: int, topk_score,
+                 topk_index, ws=None, ws_bytes: Optional[int] = None, stream=None):
+    _check(_lib.hs_topk_rows(_ptr(scores), dtype, stride, n_rows, n_cols, k, _ptr(topk_score),
+                             _ptr(topk_index), _ptr(ws), _ws_bytes(ws, ws_bytes),
+                             _stream(stream)))
 
 
 # ---------------------------------------------------------------- composition
@@ -604,3 +694,283 @@ def merge_retrieval(keys, q_req, corpus, k: int, scale=None, workflow_offsets=No
             "counts": m.counts[:nu], "inverse": m.inverse[:R],
             "topk_score": m.topk_score[:nu], "topk_index": m.topk_index[:nu],
             "n_unique": nu, "retrieval": m}
+
+
+# ---------------------------------------------------------------- row tables
+
+def _on(stream, device):
+    """(device context, stream) of a one-call operator: launches and new tensors belong
+    to `stream` (default: the device's current stream) whatever device and stream are
+    current."""
+    import torch
+    if device.type != "cuda":
+        raise TypeError("tensors must be on a GPU")
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    return torch.cuda.device(device), stream
+
+
+def _float_code(dtype, what: str) -> int:
+    import torch
+    if dtype == torch.float32:
+        return HS_F32
+    if dtype == torch.bfloat16:
+        return HS_BF16
+    raise TypeError(f"{what} must be float32 or bfloat16, not {dtype}")
+
+
+def _tensor(t, what: str, device, shape=None, dtypes=None):
+    """Checks one contiguous device tensor."""
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, not on {device}")
+    if dtypes is not None and t.dtype not in dtypes:
+        raise TypeError(f"{what} must be {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return t
+
+
+def _rows_of(t, what: str):
+    """Row stride of a 2-D tensor whose rows are contiguous."""
+    if t.dim() != 2:
+        raise ValueError(f"{what} must be 2-D")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what} must have contiguous rows")
+    if t.shape[0] > 1:
+        if t.stride(0) < t.shape[1]:
+            raise ValueError(f"{what} has overlapping rows")
+        return t.stride(0)
+    return t.shape[1]
+
+
+class RowTable:
+    """A table of rows in device memory (hs_row_table) and the tensors behind it:
+    data [rows x dim] float32 or bfloat16; float8_e4m3fn or uint8 codes with scales
+    [rows] float32; or, with group = 32, 64 or 128, packed E2M1 codes [rows x dim / 2]
+    uint8 with scales [rows x dim / group] float32 or bfloat16."""
+
+    def __init__(self, data, scales=None, group: int = 0):
+        import torch
+        if data.dim() != 2:
+            raise ValueError("data must be 2-D")
+        _tensor(data, "data", data.device)
+        rows, width = data.shape
+        f32, bf16 = torch.float32, torch.bfloat16
+        sdt = 0
+        if group:
+            _tensor(data, "data", data.device, dtypes=(torch.uint8,))
+            dim, code = 2 * width, HS_FP4_E2M1
+            if scales is None:
+                raise ValueError("a packed table needs scales")
+            if group not in (32, 64, 128) or dim % group:
+                raise ValueError(f"group {group} does not fit {dim} columns")
+            _tensor(scales, "scales", data.device, (rows, dim // group), (f32, bf16))
+            sdt = _float_code(scales.dtype, "scales")
+        else:
+            dim, code = width, dtype_code(data)
+            if code == HS_FP8_E4M3:
+                if scales is None:
+                    raise ValueError("an fp8 table needs scales")
+                _tensor(scales, "scales", data.device, (rows,), (f32,))
+            elif scales is not None:
+                raise ValueError("scales belong to fp8 and packed tables")
+        self.data, self.scales, self.group = data, scales, group
+        self.rows, self.dim, self.device = rows, dim, data.device
+        self.c = hs_row_table(_ptr(data), _ptr(scales), rows, dim, code, sdt, group)
+
+
+def pack_rows(rows, group: int = 32, scale_dtype=None, stream=None) -> RowTable:
+    """The packed 4-bit table of rows [n x dim] (float32 or bfloat16), dim a multiple of
+    group (32, 64 or 128); scale_dtype bfloat16 (the default) or float32."""
+    import torch
+    scale_dtype = torch.bfloat16 if scale_dtype is None else scale_dtype
+    if rows.dim() != 2:
+        raise ValueError("rows must be 2-D")
+    _tensor(rows, "rows", rows.device)
+    code, sdt = _float_code(rows.dtype, "rows"), _float_code(scale_dtype, "scale_dtype")
+    if group not in (32, 64, 128) or rows.shape[1] == 0 or rows.shape[1] % group:
+        raise ValueError(f"group {group} does not fit {rows.shape[1]} columns")
+    n, d = rows.shape
+    ctx, stream = _on(stream, rows.device)
+    with ctx, torch.cuda.stream(stream):
+        data = torch.empty((n, d // 2), dtype=torch.uint8, device=rows.device)
+        scales = torch.empty((n, d // group), dtype=scale_dtype, device=rows.device)
+        hs_pack_rows(rows, code, n, d, group, sdt, data, scales, stream=stream)
+    return RowTable(data, scales, group)
+
+
+def _ids(ids, device):
+    import torch
+    _tensor(ids, "ids", device, dtypes=(torch.int32, torch.int64))
+    return int(ids.dtype == torch.int64), ids.numel()
+
+
+def embed(table: RowTable, ids, scale: float = 1.0, pad_id: int = -1, out_dtype=None, out=None,
+          stream=None):
+    """Embedding lookup with scaling: scale * table[ids] for ids of any shape (int32 or
+    int64), as ids.shape + [dim] in out_dtype (default: the table's type, bfloat16 for
+    quantised tables).  Ids outside the table and pad_id give rows of zeros.  `out`:
+    a contiguous tensor for the result."""
+    import torch
+    device = table.device
+    is64, n = _ids(ids, device)
+    shape = tuple(ids.shape) + (table.dim,)
+    ctx, stream = _on(stream, device)
+    with ctx:
+        if out is None:
+            if out_dtype is None:
+                out_dtype = torch.float32 if table.c.dtype == HS_F32 else torch.bfloat16
+            with torch.cuda.stream(stream):
+                out = torch.empty(shape, dtype=out_dtype, device=device)
+        else:
+            _tensor(out, "out", device, shape, None if out_dtype is None else (out_dtype,))
+        hs_embed(table.c, ids, is64, n, scale, pad_id, out, _float_code(out.dtype, "out"),
+                 stream=stream)
+    return out
+
+
+def embed_grad(d_out, ids, rows: int, scale: float = 1.0, pad_id: int = -1, out_dtype=None,
+               out=None, accumulate: bool = False, ws=None, stream=None):
+    """Gradient of embed with respect to its table of `rows` rows: d_out is ids.shape +
+    [dim] (float32 or bfloat16), the result [rows x dim] in out_dtype (default: that of
+    d_out).  accumulate adds to `out`.  `ws`: a uint8 workspace of hs_embed_grad_bytes'
+    size to use instead of a new one."""
+    import torch
+    device = d_out.device
+    is64, n = _ids(ids, device)
+    if d_out.dim() < 1:
+        raise ValueError("d_out needs a column dimension")
+    dim = d_out.shape[-1]
+    _tensor(d_out, "d_out", device, tuple(ids.shape) + (dim,))
+    code = _float_code(d_out.dtype, "d_out")
+    if accumulate and out is None:
+        raise ValueError("accumulate needs out")
+    ctx, stream = _on(stream, device)
+    with ctx:
+        if out is None or ws is None:
+            with torch.cuda.stream(stream):
+                if out is None:
+                    out = torch.empty((rows, dim), dtype=out_dtype or d_out.dtype, device=device)
+                if ws is None:
+                    ws = torch.empty(hs_embed_grad_bytes(n, rows, dim), dtype=torch.uint8,
+                                     device=device)
+        _tensor(out, "out", device, (rows, dim), None if out_dtype is None else (out_dtype,))
+        _tensor(ws, "ws", device)
+        hs_embed_grad(d_out, code, ids, is64, n, rows, dim, scale, pad_id, int(accumulate), out,
+                      _float_code(out.dtype, "out"), ws, stream=stream)
+    return out
+
+
+def score_packed(table: RowTable, x, out_dtype=None, out=None, stream=None):
+    """Products of rows x [m x dim] (float32 or bfloat16) with every row of a packed
+    table, [m x table.rows] in out_dtype (default float32).  `out` may have a row
+    stride above table.rows."""
+    import torch
+    device = table.device
+    if table.c.dtype != HS_FP4_E2M1:
+        raise TypeError("the table must be packed (pack_rows)")
+    if x.dim() != 2:
+        raise ValueError("x must be 2-D")
+    m = x.shape[0]
+    _tensor(x, "x", device, (m, table.dim))
+    code = _float_code(x.dtype, "x")
+    ctx, stream = _on(stream, device)
+    with ctx:
+        if out is None:
+            with torch.cuda.stream(stream):
+                out = torch.empty((m, table.rows), dtype=out_dtype or torch.float32,
+                                  device=device)
+        stride = _rows_of(out, "out")
+        if out.device != device or tuple(out.shape) != (m, table.rows) or \
+                out_dtype not in (None, out.dtype):
+            raise ValueError("out does not fit the table, x and out_dtype")
+        hs_score_packed(table.c, x, code, m, out, _float_code(out.dtype, "out"), stride,
+                        stream=stream)
+    return out
+
+
+def adjust_scores(scores, allow=None, seen=None, seen_off=None, prompt_len=None, repetition=None,
+                  frequency=None, presence=None, bias_id=None, bias=None, bias_off=None, out=None,
+                  stream=None):
+    """Penalties for repeated tokens, biases and allow masks on scores [rows x cols]
+    (float32 or bfloat16; hs_adjust_scores gives the formulas).  seen [any] int32 with
+    seen_off [rows + 1] int64; prompt_len [rows] int32; repetition, frequency, presence
+    [rows] float32; bias_id [any] int32 and bias float32 with bias_off [rows + 1] int64;
+    allow: int32 words, bit c % 32 of word c / 32 for column c, [words] for all rows or
+    [rows x words].  `out` may be scores; by default a new tensor."""
+    import torch
+    device = scores.device
+    stride = _rows_of(scores, "scores")
+    code = _float_code(scores.dtype, "scores")
+    rows, cols = scores.shape
+    if (seen is None) != (seen_off is None):
+        raise ValueError("seen and seen_off belong together")
+    if not (bias_id is None) == (bias is None) == (bias_off is None):
+        raise ValueError("bias_id, bias and bias_off belong together")
+    f32, i32, i64 = (torch.float32,), (torch.int32,), (torch.int64,)
+    a = hs_adjust()
+    if seen is not None:
+        a.seen = _ptr(_tensor(seen, "seen", device, dtypes=i32))
+        a.seen_off = _ptr(_tensor(seen_off, "seen_off", device, (rows + 1,), i64))
+        a.n_seen = seen.numel()
+    if bias_id is not None:
+        a.bias_id = _ptr(_tensor(bias_id, "bias_id", device, dtypes=i32))
+        a.bias = _ptr(_tensor(bias, "bias", device, bias_id.shape, f32))
+        a.bias_off = _ptr(_tensor(bias_off, "bias_off", device, (rows + 1,), i64))
+        a.n_bias = bias_id.numel()
+    if prompt_len is not None:
+        a.prompt_len = _ptr(_tensor(prompt_len, "prompt_len", device, (rows,), i32))
+    if repetition is not None:
+        a.repetition = _ptr(_tensor(repetition, "repetition", device, (rows,), f32))
+    if frequency is not None:
+        a.frequency = _ptr(_tensor(frequency, "frequency", device, (rows,), f32))
+    if presence is not None:
+        a.presence = _ptr(_tensor(presence, "presence", device, (rows,), f32))
+    if allow is not None:
+        words = (cols + 31) // 32
+        if allow.dim() == 1:
+            _tensor(allow, "allow", device, (words,), i32)
+        else:
+            _tensor(allow, "allow", device, (rows, words), i32)
+            a.allow_stride = words
+        a.allow = _ptr(allow)
+    ctx, stream = _on(stream, device)
+    with ctx:
+        if out is None:
+            with torch.cuda.stream(stream):
+                out = torch.empty((rows, cols), dtype=scores.dtype, device=device)
+        elif out.device != device or out.shape != scores.shape or out.dtype != scores.dtype:
+            raise ValueError("out does not fit scores")
+        hs_adjust_scores(a, scores, stride, out, _rows_of(out, "out"), code, rows, cols,
+                         stream=stream)
+    return out
+
+
+def topk_rows(scores, k: int, out=None, ws=None, stream=None):
+    """The k best columns of every row of scores [rows x cols] (float32 or bfloat16):
+    (score [rows x k] float32, column [rows x k] int32), score descending, equal scores by
+    ascending column; entries of -inf and NaN are never taken, slots left are (-inf, -1).
+    `out`: the two tensors for the result, `ws`: a uint8 workspace of
+    hs_topk_rows_bytes' size."""
+    import torch
+    device = scores.device
+    stride = _rows_of(scores, "scores")
+    code = _float_code(scores.dtype, "scores")
+    rows, cols = scores.shape
+    need = hs_topk_rows_bytes(rows, cols, k) if ws is None else 0
+    ctx, stream = _on(stream, device)
+    with ctx:
+        if out is None or ws is None:
+            with torch.cuda.stream(stream):
+                if out is None:
+                    out = (torch.empty((rows, k), dtype=torch.float32, device=device),
+                           torch.empty((rows, k), dtype=torch.int32, device=device))
+                if ws is None:
+                    ws = torch.empty(need, dtype=torch.uint8, device=device)
+        _tensor(out[0], "out[0]", device, (rows, k), (torch.float32,))
+        _tensor(out[1], "out[1]", device, (rows, k), (torch.int32,))
+        _tensor(ws, "ws", device)
+        hs_topk_rows(scores, code, stride, rows, cols, k, out[0], out[1], ws, stream=stream)
+    return out

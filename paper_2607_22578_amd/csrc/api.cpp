@@ -7,13 +7,12 @@
 #include <hip/hip_runtime_api.h>
 
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <cstring>
 #include <new>
 #include <vector>
 
 #include "../../include/hs_merge.h"
+#include "status.h"
 
 namespace hs {
 size_t dedup_workspace_bytes(int64_t R);
@@ -73,27 +72,11 @@ struct hs_plan {
   size_t ws_total;
 };
 
-static thread_local char g_err[512];
-
-static hs_status fail(hs_status s, const char *fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_err, sizeof(g_err), fmt, ap);
-  va_end(ap);
-  return s;
-}
-
-static hs_status ok() {
-  g_err[0] = 0;
-  return HS_OK;
-}
-
-static bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
-
-static hs_status device_status(hipError_t e, const char *what) {
-  if (e == hipSuccess) return ok();
-  return fail(HS_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
-}
+using hs::aligned;
+using hs::device_status;
+using hs::fail;
+using hs::g_err;
+using hs::ok;
 
 extern "C" {
 

@@ -1,0 +1,551 @@
+// Gradient of the embedding lookup, dT[v] = scale * sum_{i: ids[i] = v} dO[i], by
+// tokens sorted together with their positions.
+//
+//   sort    LSD radix sort of (token, position), stable, so a token's positions come
+//           in ascending order; positions that stand for no token take the key
+//           `rows`, behind all others.  Up to kSmallMax positions in one workgroup;
+//           above, two launches per digit (counts per tile, scatter).
+//   starts  start[v] = first sorted place of token v (binary search per row).
+//   sums    the sorted places in chunks of at most 64: a wave adds up the rows of
+//           its chunk for one slice of columns, place after place, in registers, and
+//           writes a row whenever the token changes.  The work per wave does not depend
+//           on how often tokens occur.  Tokens that reach over a chunk's end leave
+//           partial sums.  The same launch writes the rows of tokens that do not occur.
+//   join    partial sums of the tokens over several chunks, in chunk order.
+// Every row's additions are thus in an order that the sizes and ids fix.
+// Floor: dO once, dT once; the keys are small beside them.
+#include "rows.h"
+
+namespace hs {
+
+namespace {
+
+constexpr int kSmallMax = 4096;      // positions that one workgroup sorts
+constexpr int kSmallWaves = 16;
+constexpr int kSortWaves = 8;        // per tile
+constexpr int kDigitBits = 9;        // most bits of a digit
+constexpr int kDigits = 1 << kDigitBits;
+static_assert(kSortWaves * 64 == kDigits, "a thread per digit");
+constexpr int kTilesMax = 128;       // tiles of the sort
+constexpr int kTileMin = 2048;       // positions that make another tile worth it
+constexpr int kChunk = 64;           // sorted places of one wave, at most
+
+struct GradWs {
+  uint32_t *tok[2], *pos[2];   // [n] each: sorted keys and positions
+  uint32_t *hist;              // [kTilesMax][kDigits]
+  uint32_t *start;             // [rows + 1]
+  float *part;                 // [2 x chunks][dim]: sums of the tokens over a chunk's
+                               // start (0) and end (1)
+};
+
+__host__ __device__ int64_t up256(int64_t x) { return (x + 255) & ~(int64_t)255; }
+
+// Places per chunk: 64, or fewer while the chunks and column slices (of 512) would
+// not give 2,048 waves (8 per CU).
+int chunk_places(int64_t n, int64_t dim) {
+  int c = kChunk;
+  while (c > 8 && (n + c - 1) / c * ((dim + 511) / 512) < 2048) c >>= 1;
+  return c;
+}
+
+size_t layout(int64_t n, int64_t rows, int64_t dim, void *base, GradWs *w) {
+  uint8_t *p = (uint8_t *)base;
+  const int64_t kb = up256(n * 4);
+  const int64_t chunks = (n + chunk_places(n, dim) - 1) / chunk_places(n, dim);
+  int64_t at = 0;
+  for (int i = 0; i < 2; ++i) {
+    if (w) w->tok[i] = (uint32_t *)(p + at);
+    at += kb;
+    if (w) w->pos[i] = (uint32_t *)(p + at);
+    at += kb;
+  }
+  if (w) w->hist = (uint32_t *)(p + at);
+  at += (int64_t)kTilesMax * kDigits * 4;
+  if (w) w->start = (uint32_t *)(p + at);
+  at += up256((rows + 1) * 4);
+  if (w) w->part = (float *)(p + at);
+  at += up256(chunks * 2 * dim * 4);
+  return (size_t)at;
+}
+
+// ---------------------------------------------------------------- sort
+
+__device__ __forceinline__ uint32_t token_key(const void *ids, int is64, int64_t i, int64_t rows,
+                                              int64_t pad) {
+  const int64_t id = load_id(ids, is64, i);
+  return (uint32_t)(id >= 0 && id < rows && id != pad ? id : rows);
+}
+
+// Orders a wave's LDS accesses (its lanes run together: only the compiler has to).
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Lanes of the wave with the same digit as this one, among the lanes in `in`.
+__device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, bool in) {
+  uint64_t m = __builtin_amdgcn_ballot_w64(in);
+  for (int b = 0; b < bits; ++b) {
+    const bool one = (d >> b) & 1u;
+    const uint64_t v = __builtin_amdgcn_ballot_w64(one);
+    m &= one ? v : ~v;
+  }
+  return m;
+}
+
+// All passes in one workgroup, keys and positions in LDS; 16 waves, each with a
+// contiguous share and its own digit counters (made exclusive over digits and waves).
+__global__ __launch_bounds__(kSmallWaves * 64) void grad_sort_small(
+    const void *__restrict__ ids, int is64, int n, int64_t rows, int64_t pad, int bits, int passes,
+    uint32_t *__restrict__ tok, uint32_t *__restrict__ pos) {
+  __shared__ uint32_t key[2][kSmallMax], val[2][kSmallMax];
+  __shared__ uint32_t cnt[kSmallWaves][kDigits];
+  __shared__ uint32_t total[kDigits];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int i = tid; i < n; i += kSmallWaves * 64) {
+    key[0][i] = token_key(ids, is64, i, rows, pad);
+    val[0][i] = (uint32_t)i;
+  }
+  const int share = ((n + kSmallWaves - 1) / kSmallWaves + 63) & ~63;
+  const int lo = wave * share, hi = lo + share < n ? lo + share : n;
+  int from = 0;
+  for (int p = 0; p < passes; ++p) {
+    const int shift = p * bits;
+    const uint32_t mask = (1u << bits) - 1u;
+    for (int i = tid; i < kSmallWaves * kDigits; i += kSmallWaves * 64) (&cnt[0][0])[i] = 0u;
+    __syncthreads();
+    for (int i = lo + lane; i < hi; i += 64) atomicAdd(&cnt[wave][(key[from][i] >> shift) & mask], 1u);
+    __syncthreads();
+    // digit totals, their exclusive scan (512 digits in the first 8 waves)
+    uint32_t mine = 0u;
+    if (tid < kDigits) {
+      for (int w = 0; w < kSmallWaves; ++w) mine += cnt[w][tid];
+      total[tid] = mine;
+    }
+    __syncthreads();
+    for (int d = 1; d < kDigits; d <<= 1) {
+      uint32_t add = 0u;
+      if (tid < kDigits && tid >= d) add = total[tid - d];
+      __syncthreads();
+      if (tid < kDigits) total[tid] += add;
+      __syncthreads();
+    }
+    if (tid < kDigits) {
+      uint32_t base = total[tid] - mine;
+      for (int w = 0; w < kSmallWaves; ++w) {
+        const uint32_t c = cnt[w][tid];
+        cnt[w][tid] = base;
+        base += c;
+      }
+    }
+    __syncthreads();
+    for (int i0 = lo; i0 < hi; i0 += 64) {
+      const int i = i0 + lane;
+      const bool in = i < hi;
+      const uint32_t k = in ? key[from][i] : 0u;
+      const uint32_t d = (k >> shift) & mask;
+      const uint64_t same = same_digit(d, bits, in);
+      if (in) {
+        const int rank = __popcll(same & ((1ull << lane) - 1ull));
+        const uint32_t at = cnt[wave][d] + rank;
+        key[from ^ 1][at] = k;
+        val[from ^ 1][at] = val[from][i];
+      }
+      wave_fence();
+      if (in && (same >> lane) == 1ull) cnt[wave][d] += (uint32_t)__popcll(same);
+      wave_fence();
+    }
+    from ^= 1;
+    __syncthreads();
+  }
+  for (int i = tid; i < n; i += kSmallWaves * 64) {
+    tok[i] = key[from][i];
+    pos[i] = val[from][i];
+  }
+}
+
+// Digit counts of one tile; the first pass makes the keys from the ids.
+template <bool FIRST>
+__global__ __launch_bounds__(kSortWaves * 64) void grad_count(
+    const void *__restrict__ ids, int is64, const uint32_t *__restrict__ tok, int64_t n,
+    int64_t tile, int64_t rows, int64_t pad, int bits, int shift, uint32_t *__restrict__ hist) {
+  __shared__ uint32_t cnt[kDigits];
+  cnt[threadIdx.x] = 0u;
+  __syncthreads();
+  const int64_t lo = (int64_t)blockIdx.x * tile, hi = lo + tile < n ? lo + tile : n;
+  const uint32_t mask = (1u << bits) - 1u;
+  for (int64_t i = lo + threadIdx.x; i < hi; i += kSortWaves * 64) {
+    const uint32_t k = FIRST ? token_key(ids, is64, i, rows, pad) : tok[i];
+    atomicAdd(&cnt[(k >> shift) & mask], 1u);
+  }
+  __syncthreads();
+  hist[(int64_t)blockIdx.x * kDigits + threadIdx.x] = cnt[threadIdx.x];
+}
+
+// Stable scatter of one tile.  The tile's first place of each digit comes straight
+// from the counts of all tiles (at most 128 reads per digit and workgroup).
+template <bool FIRST>
+__global__ __launch_bounds__(kSortWaves * 64) void grad_scatter(
+    const void *__restrict__ ids, int is64, const uint32_t *__restrict__ tok,
+    const uint32_t *__restrict__ pos, int64_t n, int64_t tile, int tiles, int64_t rows,
+    int64_t pad, int bits, int shift, const uint32_t *__restrict__ hist,
+    uint32_t *__restrict__ tok_out, uint32_t *__restrict__ pos_out) {
+  __shared__ uint32_t cnt[kSortWaves][kDigits];
+  __shared__ uint32_t total[kDigits];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint32_t mask = (1u << bits) - 1u;
+  const int64_t lo = (int64_t)blockIdx.x * tile, hi = lo + tile < n ? lo + tile : n;
+  const int64_t share = tile / kSortWaves;   // (a multiple of 64)
+  const int64_t wlo = lo + wave * share < hi ? lo + wave * share : hi;
+  const int64_t whi = wlo + share < hi ? wlo + share : hi;
+  for (int w = 0; w < kSortWaves; ++w) cnt[w][tid] = 0u;
+  __syncthreads();
+  for (int64_t i = wlo + lane; i < whi; i += 64) {
+    const uint32_t k = FIRST ? token_key(ids, is64, i, rows, pad) : tok[i];
+    atomicAdd(&cnt[wave][(k >> shift) & mask], 1u);
+  }
+  uint32_t before = 0u, all = 0u;
+#pragma unroll 8
+  for (int t = 0; t < tiles; ++t) {
+    const uint32_t c = hist[(int64_t)t * kDigits + tid];
+    if (t < (int)blockIdx.x) before += c;
+    all += c;
+  }
+  total[tid] = all;
+  __syncthreads();
+  for (int d = 1; d < kDigits; d <<= 1) {
+    const uint32_t add = tid >= d ? total[tid - d] : 0u;
+    __syncthreads();
+    total[tid] += add;
+    __syncthreads();
+  }
+  uint32_t base = total[tid] - all + before;
+  for (int w = 0; w < kSortWaves; ++w) {
+    const uint32_t c = cnt[w][tid];
+    cnt[w][tid] = base;
+    base += c;
+  }
+  __syncthreads();
+  for (int64_t i0 = wlo; i0 < whi; i0 += 64) {
+    const int64_t i = i0 + lane;
+    const bool in = i < whi;
+    uint32_t k = 0u, v = 0u;
+    if (in) {
+      k = FIRST ? token_key(ids, is64, i, rows, pad) : tok[i];
+      v = FIRST ? (uint32_t)i : pos[i];
+    }
+    const uint32_t d = (k >> shift) & mask;
+    const uint64_t same = same_digit(d, bits, in);
+    if (in) {
+      const uint32_t at = cnt[wave][d] + (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
+      tok_out[at] = k;
+      pos_out[at] = v;
+    }
+    wave_fence();
+    if (in && (same >> lane) == 1ull) cnt[wave][d] += (uint32_t)__popcll(same);
+    wave_fence();
+  }
+}
+
+// start[v] for v <= rows: the first sorted place whose token is v or above.
+__global__ __launch_bounds__(256) void grad_starts(const uint32_t *__restrict__ tok, int64_t n,
+                                                   int64_t rows, uint32_t *__restrict__ start) {
+  for (int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x; v <= rows;
+       v += (int64_t)gridDim.x * 256) {
+    int64_t a = 0, b = n;
+    while (a < b) {
+      const int64_t m = (a + b) >> 1;
+      if (tok[m] < (uint32_t)v)
+        a = m + 1;
+      else
+        b = m;
+    }
+    start[v] = (uint32_t)a;
+  }
+}
+
+// ---------------------------------------------------------------- sums
+//
+// V columns per lane and slice: consecutive ones where 16-byte accesses fit (WIDE),
+// else 64 apart.
+template <int DT, bool WIDE>
+struct Slice {
+  static constexpr int V = DT == HS_F32 ? 4 : 8;
+  static constexpr int kCols = 64 * V;
+
+  __device__ static __forceinline__ void load(const uint8_t *row, int col0, int lane, int dim,
+                                              float *v) {
+    if constexpr (WIDE) {
+      const int c = col0 + lane * V;
+      if (c < dim) {
+        RawCols<DT, V> raw;
+        raw.load(row, c);
+        raw.decode(v);
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = 0.0f;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int c = col0 + j * 64 + lane;
+        v[j] = c < dim ? load_col<DT>(row, c) : 0.0f;
+      }
+    }
+  }
+
+  // partial sums keep the lane's columns in the same places
+  __device__ static __forceinline__ void part(float *row, int col0, int lane, int dim,
+                                              const float *v) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int c = WIDE ? col0 + lane * V + j : col0 + j * 64 + lane;
+      if (c < dim) row[c] = v[j];
+    }
+  }
+
+  template <int OT>
+  __device__ static __forceinline__ void write(uint8_t *table, int64_t r, int col0, int lane,
+                                               int dim, int add, const float *v) {
+    constexpr int OB = OT == HS_F32 ? 4 : 2;
+    uint8_t *row = table + r * (int64_t)dim * OB;
+    if constexpr (WIDE) {
+      const int c = col0 + lane * V;
+      if (c >= dim) return;
+      float o[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) o[j] = v[j];
+      if (add) {
+        RawCols<OT, V> raw;
+        float old[V];
+        raw.load(row, c);
+        raw.decode(old);
+#pragma unroll
+        for (int j = 0; j < V; ++j) o[j] += old[j];
+      }
+      if constexpr (OT == HS_F32) {
+#pragma unroll
+        for (int j = 0; j < V; j += 4)
+          __builtin_nontemporal_store(round_cols<HS_F32, 4>(o + j),
+                                      (u32x4v_t *)(row + (int64_t)(c + j) * 4));
+      } else if constexpr (V == 8) {
+        __builtin_nontemporal_store(round_cols<HS_BF16, 8>(o),
+                                    (u32x4v_t *)(row + (int64_t)c * 2));
+      } else {
+        uint2 w;
+        w.x = f32_to_bf16x2(o[0], o[1]);
+        w.y = f32_to_bf16x2(o[2], o[3]);
+        *(uint2 *)(row + (int64_t)c * 2) = w;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int c = col0 + j * 64 + lane;
+        if (c < dim) store_col<OT>(row, c, add ? v[j] + load_col<OT>(row, c) : v[j]);
+      }
+    }
+  }
+};
+
+template <int DT, int OT, bool WIDE>
+__global__ __launch_bounds__(256) void grad_sums(
+    const uint8_t *__restrict__ grad, const uint32_t *__restrict__ tok,
+    const uint32_t *__restrict__ pos, const uint32_t *__restrict__ start, int64_t n, int64_t rows,
+    int dim, int places, int64_t chunks, int slices, int64_t sum_blocks, float scale, int add,
+    float *__restrict__ part, uint8_t *__restrict__ table) {
+  using S = Slice<DT, WIDE>;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if ((int64_t)blockIdx.x >= sum_blocks) {
+    // rows of tokens that do not occur: a wave per row and slice
+    float zero[S::V] = {};
+    const int64_t all = rows * slices;
+    for (int64_t t = ((int64_t)blockIdx.x - sum_blocks) * 4 + wave; t < all;
+         t += ((int64_t)gridDim.x - sum_blocks) * 4) {
+      const int64_t r = t / slices;
+      if (start[r] == start[r + 1])
+        S::template write<OT>(table, r, (int)(t - r * slices) * S::kCols, lane, dim, 0, zero);
+    }
+    return;
+  }
+  const int64_t task = (int64_t)blockIdx.x * 4 + wave;
+  if (task >= chunks * slices) return;
+  const int64_t c = task / slices;
+  const int col0 = (int)(task - c * slices) * S::kCols;
+  const int64_t lo = c * places;
+  const int m = (int)(n - lo < places ? n - lo : places);
+  const uint32_t none = (uint32_t)rows;
+  const uint32_t my_tok = lane < m ? tok[lo + lane] : none;
+  const uint32_t my_pos = lane < m ? pos[lo + lane] : 0u;
+  const uint32_t prev = lo > 0 ? tok[lo - 1] : none;
+  const uint32_t next = lo + m < n ? tok[lo + m] : none;
+  const int64_t gb = row_bytes<DT>(dim);
+  float acc[S::V] = {};
+  uint32_t cur = __builtin_amdgcn_readlane(my_tok, 0);
+  bool head = cur == prev;   // the current token began in an earlier chunk
+  constexpr int U = 8;
+  for (int i0 = 0; i0 < m; i0 += U) {
+    float v[U][S::V];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u < m ? i0 + u : m - 1;
+      const int64_t at = (int64_t)(uint32_t)__builtin_amdgcn_readlane(my_pos, i);
+      S::load(grad + at * gb, col0, lane, dim, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i0 + u < m) {
+        const uint32_t t = __builtin_amdgcn_readlane(my_tok, i0 + u);
+        if (t != cur) {
+          if (head) {
+            S::part(part + (c * 2) * dim, col0, lane, dim, acc);
+          } else {
+#pragma unroll
+            for (int j = 0; j < S::V; ++j) acc[j] *= scale;
+            S::template write<OT>(table, cur, col0, lane, dim, add, acc);
+          }
+#pragma unroll
+          for (int j = 0; j < S::V; ++j) acc[j] = 0.0f;
+          cur = t;
+          head = false;
+          if (cur == none) return;   // (only positions without a token are left)
+        }
+        if (cur == none) return;
+#pragma unroll
+        for (int j = 0; j < S::V; ++j) acc[j] += v[u][j];
+      }
+    }
+  }
+  if (cur == none) return;
+  if (head) {
+    S::part(part + (c * 2) * dim, col0, lane, dim, acc);
+  } else if (cur == next) {
+    S::part(part + (c * 2 + 1) * dim, col0, lane, dim, acc);
+  } else {
+#pragma unroll
+    for (int j = 0; j < S::V; ++j) acc[j] *= scale;
+    S::template write<OT>(table, cur, col0, lane, dim, add, acc);
+  }
+}
+
+// Tokens over several chunks: the workgroup of the chunk where the token begins adds
+// that chunk's partial sum and those of the following chunks, 64 columns at a time,
+// four contiguous shares of the chunks by four waves, joined in order.
+template <int OT>
+__global__ __launch_bounds__(256) void grad_join(
+    const uint32_t *__restrict__ tok, const uint32_t *__restrict__ start, int64_t n, int64_t rows,
+    int dim, int places, int col_blocks, int64_t tasks, float scale, int add,
+    const float *__restrict__ part,
+    uint8_t *__restrict__ table) {
+  __shared__ float sums[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
+    const int64_t c = task / col_blocks;
+    const int col = (int)(task - c * col_blocks) * 64 + lane;
+    const int64_t end = (c + 1) * places;   // < n: the last chunk has no task
+    const uint32_t t = tok[end - 1];
+    if (t == (uint32_t)rows || tok[end] != t) continue;
+    const int64_t first = start[t], last = (int64_t)start[t + 1] - 1;
+    if (first < c * places) continue;   // began earlier: that chunk's task joins it
+    // chunks c + 1 .. c1 hold the token's other sums
+    const int64_t c1 = last / places, count = c1 - c, share = (count + 3) / 4;
+    const int64_t a = c + 1 + wave * share, b = a + share < c1 + 1 ? a + share : c1 + 1;
+    float acc = 0.0f;
+    if (col < dim) {
+      if (wave == 0) acc = part[(c * 2 + 1) * dim + col];
+#pragma unroll 8
+      for (int64_t k = a; k < b; ++k) acc += part[k * 2 * dim + col];
+    }
+    sums[wave][lane] = acc;
+    __syncthreads();
+    if (wave == 0 && col < dim) {
+      float v = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
+      v *= scale;
+      uint8_t *row = table + (int64_t)t * dim * (OT == HS_F32 ? 4 : 2);
+      store_col<OT>(row, col, add ? v + load_col<OT>(row, col) : v);
+    }
+    __syncthreads();
+  }
+}
+
+template <int DT, int OT>
+hipError_t launch_sums(const GradWs &w, int side, const void *grad, int64_t n, int64_t rows,
+                       int64_t dim, float scale, int add, void *table, hipStream_t st) {
+  constexpr int V = DT == HS_F32 ? 4 : 8;
+  const int places = chunk_places(n, dim);
+  const int64_t chunks = (n + places - 1) / places;
+  const int slices = (int)((dim + 64 * V - 1) / (64 * V));
+  const bool wide = dim % V == 0 && ((uintptr_t)grad % 16) == 0 && ((uintptr_t)table % 16) == 0;
+  const int64_t sum_blocks = (chunks * slices + 3) / 4;
+  int64_t zero_blocks = add ? 0 : (rows * slices + 3) / 4;
+  if (zero_blocks > 4096) zero_blocks = 4096;
+  hipLaunchKernelGGL((wide ? grad_sums<DT, OT, true> : grad_sums<DT, OT, false>),
+                     dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, st,
+                     (const uint8_t *)grad, w.tok[side], w.pos[side], w.start, n, rows, (int)dim,
+                     places, chunks, slices, sum_blocks, scale, add, w.part, (uint8_t *)table);
+  const int col_blocks = (int)((dim + 63) / 64);
+  const int64_t tasks = (chunks - 1) * col_blocks;
+  if (tasks > 0)
+    hipLaunchKernelGGL(grad_join<OT>, dim3((unsigned)(tasks < 65536 ? tasks : 65536)), dim3(256),
+                       0, st, w.tok[side], w.start, n, rows, (int)dim, places, col_blocks, tasks,
+                       scale, add, w.part, (uint8_t *)table);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t embed_grad_workspace_bytes(int64_t n, int64_t rows, int64_t dim) {
+  return layout(n, rows, dim, nullptr, nullptr);
+}
+
+hipError_t launch_embed_grad(const void *grad, int grad_dtype, const void *ids, int is64,
+                             int64_t n, int64_t rows, int64_t dim, float scale, int64_t pad,
+                             int add, void *table, int table_dtype, void *ws, hipStream_t st) {
+  if (rows <= 0 || (n <= 0 && add)) return hipSuccess;
+  GradWs w;
+  layout(n, rows, dim, ws, &w);
+  int key_bits = 1;   // of rows + 1 keys
+  while (((int64_t)1 << key_bits) <= rows) ++key_bits;
+  const int passes = (key_bits + kDigitBits - 1) / kDigitBits;
+  const int bits = (key_bits + passes - 1) / passes;
+  int side = 0;
+  if (n > 0 && n <= kSmallMax) {
+    hipLaunchKernelGGL(grad_sort_small, dim3(1), dim3(kSmallWaves * 64), 0, st, ids, is64, (int)n,
+                       rows, pad, bits, passes, w.tok[0], w.pos[0]);
+  } else if (n > 0) {
+    int64_t tiles = (n + kTileMin - 1) / kTileMin;
+    if (tiles > kTilesMax) tiles = kTilesMax;
+    int64_t tile = (n + tiles - 1) / tiles;
+    tile = (tile + kSortWaves * 64 - 1) / (kSortWaves * 64) * (kSortWaves * 64);
+    tiles = (n + tile - 1) / tile;
+    const dim3 g((unsigned)tiles), b(kSortWaves * 64);
+    for (int p = 0; p < passes; ++p) {
+      const int shift = p * bits;
+      if (p == 0) {
+        hipLaunchKernelGGL(grad_count<true>, g, b, 0, st, ids, is64, nullptr, n, tile, rows, pad,
+                           bits, shift, w.hist);
+        hipLaunchKernelGGL(grad_scatter<true>, g, b, 0, st, ids, is64, nullptr, nullptr, n, tile,
+                           (int)tiles, rows, pad, bits, shift, w.hist, w.tok[0], w.pos[0]);
+      } else {
+        hipLaunchKernelGGL(grad_count<false>, g, b, 0, st, ids, is64, w.tok[side], n, tile, rows,
+                           pad, bits, shift, w.hist);
+        hipLaunchKernelGGL(grad_scatter<false>, g, b, 0, st, ids, is64, w.tok[side], w.pos[side],
+                           n, tile, (int)tiles, rows, pad, bits, shift, w.hist, w.tok[side ^ 1],
+                           w.pos[side ^ 1]);
+        side ^= 1;
+      }
+    }
+  }
+  int64_t blocks = (rows + 256) / 256;
+  if (blocks > 4096) blocks = 4096;
+  hipLaunchKernelGGL(grad_starts, dim3((unsigned)blocks), dim3(256), 0, st, w.tok[side], n, rows,
+                     w.start);
+  if (grad_dtype == HS_F32)
+    return table_dtype == HS_F32
+               ? launch_sums<HS_F32, HS_F32>(w, side, grad, n, rows, dim, scale, add, table, st)
+               : launch_sums<HS_F32, HS_BF16>(w, side, grad, n, rows, dim, scale, add, table, st);
+  return table_dtype == HS_F32
+             ? launch_sums<HS_BF16, HS_F32>(w, side, grad, n, rows, dim, scale, add, table, st)
+             : launch_sums<HS_BF16, HS_BF16>(w, side, grad, n, rows, dim, scale, add, table, st);
+}
+
+}  // namespace hs
