@@ -574,6 +574,70 @@ class MergedRetrieval:
                         stream=stream)
         self.deliver(stream)
 
+    # ------------------------------------------------ packed 4-bit corpus
+
+    def enable_packed(self, batch: int = 64):
+        """Allocates the scores, masks and workspace of run_packed: `batch` distinct
+        queries are scored at a time, [batch x n_corpus] fp32 scores (rows padded to
+        128 bytes)."""
+        import torch
+        if batch < 1:
+            raise ValueError("batch must be at least 1")
+        dev = self.ws.device
+        self.packed_batch = max(min(batch, self.R), 1)
+        self.packed_stride = max((self.N + 31) // 32 * 32, 32)
+        self.packed_scores = torch.empty((self.packed_batch, self.packed_stride),
+                                         dtype=torch.float32, device=dev)
+        self.packed_allow = torch.empty((max(self.R, 1), max((self.N + 31) // 32, 1)),
+                                        dtype=torch.int32, device=dev)
+        self.packed_ws = torch.empty(hs_topk_rows_bytes(self.packed_batch, self.N, self.k),
+                                     dtype=torch.uint8, device=dev)
+
+    def run_packed(self, keys, q_req, table: "RowTable", allow=None, stream=None):
+        """The whole window over a corpus packed into four bits (RowTable): dedup ->
+        representative rows -> scores of the distinct queries with every chunk -> chunks
+        that are not allowed set to -inf -> top-k -> delivery.  `allow` (int32 words, bit
+        c % 32 of word c / 32 for chunk c): [words] for the window, or [R x words] per
+        request (a filter is part of what makes two requests equal: the mask of a
+        group is that of its first request).  Reads the distinct count on the host (one
+        synchronisation).  A request with fewer than k allowed chunks has (-inf, -1) in
+        the slots left."""
+        if (table.rows, table.dim) != (self.N, self.d):
+            raise ValueError(f"a table of {table.rows} x {table.dim} for a corpus of "
+                             f"{self.N} x {self.d}")
+        if not hasattr(self, "packed_scores"):
+            self.enable_packed()
+        words = (self.N + 31) // 32
+        nu = self.dedup(keys, stream, host_count=True)
+        hs_scatter(q_req, self.R, self.q_row_bytes, self.first_index, 0, self.R, self.n_unique,
+                   self.q_unique, stream=stream)
+        adj = hs_adjust()
+        if allow is not None and words > 0:
+            if tuple(allow.shape) not in ((words,), (self.R, words)):
+                raise ValueError(f"allow has shape {tuple(allow.shape)}, not ({words},) or "
+                                 f"({self.R}, {words})")
+            _tensor(allow, "allow", self.ws.device, dtypes=(_torch.int32,))
+            adj.allow = _ptr(allow)
+            if allow.dim() == 2:
+                hs_scatter(allow, self.R, words * 4, self.first_index, 0, self.R, self.n_unique,
+                           self.packed_allow, stream=stream)
+                adj.allow_stride = words
+        for b0 in range(0, nu, self.packed_batch):
+            nb = min(self.packed_batch, nu - b0)
+            q = self.q_unique.data_ptr() + b0 * self.q_row_bytes
+            hs_score_packed(table.c, q, self.qdt, nb, self.packed_scores, HS_F32,
+                            self.packed_stride, stream=stream)
+            if adj.allow:
+                if adj.allow_stride:
+                    adj.allow = self.packed_allow.data_ptr() + b0 * words * 4
+                hs_adjust_scores(adj, self.packed_scores, self.packed_stride, self.packed_scores,
+                                 self.packed_stride, HS_F32, nb, self.N, stream=stream)
+            hs_topk_rows(self.packed_scores, HS_F32, self.packed_stride, nb, self.N, self.k,
+                         self.topk_score.data_ptr() + b0 * self.k * 4,
+                         self.topk_index.data_ptr() + b0 * self.k * 4, self.packed_ws,
+                         stream=stream)
+        self.deliver(stream)
+
     # ------------------------------------------------ ready-queue priorities
 
     def priority(self, phi, s_hat, heavy=None, alpha=1.0, gamma=1.0, delta=0.0, eps=1e-6,
