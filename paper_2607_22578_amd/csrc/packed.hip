@@ -8,21 +8,28 @@
 // and added in fp32.  fp32 rows of x are split into three bf16 parts (the top 8, the
 // next 8 and the last 8 significant bits: exact).
 //
-// A wave loads 16 bytes (32 columns) per lane: lane l has row l % 16 and piece l / 16 of
-// 128 columns.  One MFMA takes 8 columns from each of the four lane groups, so without
-// more it would mix the four pieces: right for groups of 128.  For groups of 64 and 32
-// the pieces' words are exchanged between the lane groups (two swaps of lane halves,
-// two more of lane quarters for 32), and x is read in the same order.
-// Floor: the table, read once.
+// A wave takes 256 columns of its table rows at a time: lane l has row l % 16 and the
+// 32 bytes (64 columns) l / 16 of the 128, so each row's segment is a whole cache
+// line.  (64-byte segments, 128 columns at a time, reached 3.3 TB/s without any
+// arithmetic.)  One MFMA takes 8 columns from each of the four lane quarters, so
+// without more it would mix the four pieces.  The pieces' words are exchanged between
+// the quarters (swaps of halves, then of quarters; for groups of 128 columns halves
+// alone), and x, staged in LDS, is read in the same order.
+// Floor: the table, read once.  24 bf16 rows x 1M x 768, group 64 (504 MB): 105 us, 4.8
+// TB/s; one row x 32,000 x 4,096, group 32 (74 MB): 18 us, 4.1 TB/s (a plain copy of that
+// size reads at 6).
 #include "rows.h"
 
 namespace hs {
+
+int persistent_grid();
 
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
-constexpr int kNT = 4;   // 16-row tiles of the table per wave
+constexpr int kBlock = 256;            // columns per step of a wave
+constexpr int kStageMax = 56 * 1024;   // LDS bytes of staged x
 
 __device__ __forceinline__ bf16x8_t decode_codes(uint32_t w) {
   bf16x8_t b;
@@ -49,199 +56,320 @@ __device__ __forceinline__ void swap_quarters(uint32_t &a, uint32_t &b) {
   b = r[1];
 }
 
-// After the exchange, word j of lane group p holds columns
-// piece_of(j, p) * 32 + word_of(j, p) * 8 .. + 8 of the 128, all of word j within
-// one group of columns.
+// Exchanges four words (8 columns each) of every quarter's piece.  Afterwards word j
+// of quarter p is word sub_of(j, p) of the piece piece_of(j, p): one piece for all
+// quarters (groups of 32 and 64 columns), or one of two neighbouring pieces (128).
 template <int GROUP>
 __device__ __forceinline__ void exchange(uint32_t *w) {
-  if constexpr (GROUP <= 64) {
-    swap_halves(w[0], w[1]);
-    swap_halves(w[2], w[3]);
-  }
-  if constexpr (GROUP == 32) {
+  swap_halves(w[0], w[1]);
+  swap_halves(w[2], w[3]);
+  if constexpr (GROUP < 128) {
     swap_quarters(w[0], w[2]);
     swap_quarters(w[1], w[3]);
   }
 }
 
 template <int GROUP>
-__device__ __forceinline__ int first_col(int j, int p) {
-  if constexpr (GROUP == 128) return p * 32 + j * 8;
-  // halves exchanged: words 0, 2 hold pieces 0 and 1, words 1, 3 pieces 2 and 3
-  if constexpr (GROUP == 64) return ((j & 1) * 2 + (p & 1)) * 32 + ((j & 2) + (p >> 1)) * 8;
-  // quarters too: words 0, 2, 1, 3 hold pieces 0, 1, 2, 3, their words in the order 0, 2, 1, 3
-  return ((j & 1) * 2 + (j >> 1)) * 32 + ((p & 1) * 2 + (p >> 1)) * 8;
+__device__ __forceinline__ int piece_of(int j, int p) {
+  return GROUP < 128 ? (j & 1) * 2 + (j >> 1) : (j & 1) * 2 + (p & 1);
 }
 
-// Group (of the 128 / GROUP in the block) that word j belongs to.
 template <int GROUP>
-__device__ __forceinline__ constexpr int group_of(int j) {
-  return GROUP == 128 ? 0 : GROUP == 64 ? (j & 1) : (j & 1) * 2 + (j >> 1);
+__device__ __forceinline__ int sub_of(int j, int p) {
+  return GROUP < 128 ? (p & 1) * 2 + (p >> 1) : (j & 2) + (p >> 1);
 }
 
-// The eight columns of x for one lane and MFMA, as PARTS bf16 vectors.
-template <int XT, int PARTS>
-__device__ __forceinline__ void load_x(const uint8_t *row, int col, bool in, bf16x8_t *part) {
-  if constexpr (XT == HS_BF16) {
-    part[0] = in ? *(const bf16x8_t *)(row + (int64_t)col * 2) : bf16x8_t{};
-  } else {
-    uint32_t h[8] = {};
-    if (in) {
-      RawCols<HS_F32, 8> raw;
-      raw.load(row, col);
+// Group (of the block's 256 / GROUP) of word j in half h of the pieces.
+template <int GROUP>
+constexpr __host__ __device__ int group_of(int h, int j) {
+  const int piece = (j & 1) * 2 + (GROUP < 128 ? j >> 1 : 0);
+  return (piece * 64 + h * 32) / GROUP;
+}
+
+// How the scales are read: a block's at once (bf16, no columns past the last), or one
+// by one (other tables).  Every load is unconditional, at a clamped place where it
+// would lie outside: with loads under conditions the compiler cannot count those in
+// flight, and waits for the next block's before it multiplies the present one.
+enum ScaleMode { kBf16Whole, kBf16Each, kF32Each };
+
+// The 256 columns of 16 NT table rows, as loaded.
+template <int GROUP, int NT, int MODE>
+struct Block {
+  static constexpr int NG = kBlock / GROUP;
+  uint32_t w[NT][2][4];                             // a lane's 64 codes of one row, in halves
+  uint32_t s[NT][MODE == kBf16Whole ? NG / 2 : NG];   // the row's scales, bf16 in pairs
+
+  // kb: block; row, srow: the lane's table rows and their scales; p: its quarter
+  __device__ __forceinline__ void load(int kb, int dim, const uint8_t *const *row,
+                                       const uint8_t *const *srow, int p) {
+    const int c0 = kb * kBlock;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] = raw.w[i];
-    }
-    uint32_t w[3][4];
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      // truncation, so that nothing overflows; each rest is exact
-      uint32_t t[3][2];
+      for (int h = 0; h < 2; ++h) {
+        int c = c0 + p * 64 + h * 32;
+        if (MODE != kBf16Whole) c = c < dim ? c : 0;
+        const u32x4v_t v = *(const u32x4v_t *)(row[t] + c / 2);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float f = __uint_as_float(h[2 * i + e]);
+        for (int j = 0; j < 4; ++j) w[t][h][j] = v[j];
+      }
+    const int g0 = kb * NG;
 #pragma unroll
-        for (int p = 0; p < 3; ++p) {
-          t[p][e] = __float_as_uint(f) & 0xFFFF0000u;
-          f -= __uint_as_float(t[p][e]);
+    for (int t = 0; t < NT; ++t) {
+      if constexpr (MODE == kBf16Whole) {
+        __builtin_memcpy(s[t], srow[t] + g0 * 2, NG * 2);   // (aligned to 2 bytes only)
+      } else {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          const int at = c0 + g * GROUP < dim ? g0 + g : 0;
+          s[t][g] = MODE == kF32Each ? ((const uint32_t *)srow[t])[at]
+                                     : ((const uint16_t *)srow[t])[at];
         }
       }
+    }
+  }
+
+  // Codes of columns past the last become 0 (their scales are finite or not at all
+  // used elsewhere: group scales of the row's first group).
+  __device__ __forceinline__ void clear(int kb, int dim, int p) {
+    if constexpr (MODE != kBf16Whole) {
 #pragma unroll
-      for (int p = 0; p < 3; ++p) w[p][i] = (t[p][0] >> 16) | t[p][1];
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const bool in = kb * kBlock + p * 64 + h * 32 < dim;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) w[t][h][j] = in ? w[t][h][j] : 0u;
+        }
+    }
+  }
+
+  __device__ __forceinline__ float scale(int t, int g) const {
+    if constexpr (MODE == kBf16Whole)
+      return __uint_as_float(g & 1 ? s[t][g / 2] & 0xFFFF0000u : s[t][g / 2] << 16);
+    return __uint_as_float(MODE == kBf16Each ? s[t][g] << 16 : s[t][g]);
+  }
+
+  // xs: the lane's MT rows of staged x at the block's first column; xq: bytes between
+  // the parts.
+  template <int MT, int PARTS>
+  __device__ __forceinline__ void add(const uint8_t *const *xs, int xq, int p,
+                                      f32x4_t (*tot)[MT]) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      exchange<GROUP>(w[t][0]);
+      exchange<GROUP>(w[t][1]);
     }
 #pragma unroll
-    for (int p = 0; p < 3; ++p)
-      part[p] = __builtin_bit_cast(bf16x8_t, u32x4v_t{w[p][0], w[p][1], w[p][2], w[p][3]});
+    for (int g = 0; g < NG; ++g) {
+      f32x4_t acc[NT][MT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[t][m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (group_of<GROUP>(h, j) != g) continue;
+          const int col = piece_of<GROUP>(j, p) * 64 + h * 32 + sub_of<GROUP>(j, p) * 8;
+          bf16x8_t xa[MT][PARTS];
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q)
+              xa[m][q] = *(const bf16x8_t *)(xs[m] + q * xq + col * 2);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const bf16x8_t b = decode_codes(w[t][h][j]);
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+              for (int q = PARTS - 1; q >= 0; --q)   // (small parts first)
+                acc[t][m] =
+                    __builtin_amdgcn_mfma_f32_16x16x32_bf16(xa[m][q], b, acc[t][m], 0, 0, 0);
+          }
+        }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const float sc = scale(t, g);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) tot[t][m][i] = __builtin_fmaf(sc, acc[t][m][i], tot[t][m][i]);
+      }
+    }
+  }
+};
+
+// Stages columns [c0, c0 + cols) of rows [m0, m0 + m) of x in LDS, zeros past the
+// last column; fp32 as three bf16 parts (truncated, so that nothing overflows; each
+// rest is exact).  cols is a multiple of 8.
+template <int XT>
+__device__ __forceinline__ void stage_x(const uint8_t *x, int64_t m0, int m, int dim, int c0,
+                                        int cols, int row_bytes, int part_bytes, uint8_t *lds) {
+  const int vecs = cols / 8;
+  for (int i = threadIdx.x; i < m * vecs; i += 256) {
+    const int r = i / vecs, c = (i - r * vecs) * 8;
+    uint8_t *to = lds + r * row_bytes + c * 2;
+    const bool in = c0 + c < dim;
+    const int64_t at = (m0 + r) * dim + c0 + c;
+    if constexpr (XT == HS_BF16) {
+      u32x4v_t v = {0u, 0u, 0u, 0u};
+      if (in) v = *(const u32x4v_t *)(x + at * 2);
+      *(u32x4v_t *)to = v;
+    } else {
+      uint32_t h[8] = {};
+      if (in) {
+        RawCols<HS_F32, 8> raw;
+        raw.load(x, at);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] = raw.w[e];
+      }
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        u32x4v_t v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t top = h[e] & 0xFFFF0000u;
+          h[e] = __float_as_uint(__uint_as_float(h[e]) - __uint_as_float(top));
+          if (e & 1)
+            v[e / 2] |= top;
+          else
+            v[e / 2] = top >> 16;
+        }
+        *(u32x4v_t *)(to + q * part_bytes) = v;
+      }
+    }
   }
 }
 
-// One workgroup of four waves: KS of them share the columns (their sums are joined in
-// LDS, in wave order), 4 / KS have 64 table rows each.  MT tiles of 16 rows of x.
-template <int XT, int GROUP, int MT>
-__global__ __launch_bounds__(256) void score_packed_kernel(
-    const uint8_t *__restrict__ codes, const void *__restrict__ scales, int scale_bf16,
-    int64_t rows, int dim, const uint8_t *__restrict__ x, int64_t n_x, int ks, int64_t row_blocks,
+// Workgroups of four waves that loop over items: ks of the waves share the columns
+// (block kb goes to wave kb % ks; their sums are joined in LDS, in wave order), 4 / ks
+// have 16 NT table rows each.  MT tiles of 16 rows of x, staged `chunk` columns at a
+// time, once if that is all of them.  The next block's loads, also those of the next
+// item's first, are in flight while a block is multiplied.
+template <int XT, int GROUP, int MT, int NT, int MODE>
+__global__ __launch_bounds__(256, MT == 1 ? 4 : 2) void score_packed_kernel(
+    const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t rows, int dim,
+    const uint8_t *__restrict__ x, int64_t n_x, int ks, int chunk, int64_t row_blocks,
     int64_t items, void *__restrict__ out, int out_f32, int64_t out_stride) {
   constexpr int PARTS = XT == HS_F32 ? 3 : 1;
-  constexpr int XB = XT == HS_F32 ? 4 : 2;
-  constexpr int NG = 128 / GROUP;
-  __shared__ f32x4_t joined[3][kNT * MT][64];
+  extern __shared__ __align__(16) uint8_t lds[];
+  f32x4_t *joined = (f32x4_t *)lds;   // [3][NT * MT][64] where ks > 1
+  uint8_t *xs = lds + (ks > 1 ? 3 * NT * MT * 64 * 16 : 0);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int i16 = lane & 15, p = lane >> 4;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int64_t mb = item / row_blocks;
-    const int64_t rb = item - mb * row_blocks;
-    const int64_t n0 = (rb * (4 / ks) + wave / ks) * (16 * kNT);
-    const int64_t m0 = mb * (16 * MT);
-    const int part_of = wave % ks;
-    const int blocks = (dim + 127) / 128;
-    const int k0 = part_of * blocks / ks, k1 = (part_of + 1) * blocks / ks;
-    const int64_t cb = dim / 2, groups = dim / GROUP;
-    f32x4_t tot[kNT][MT];
-  #pragma unroll
-    for (int t = 0; t < kNT; ++t)
-  #pragma unroll
-      for (int m = 0; m < MT; ++m) tot[t][m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    const uint8_t *row[kNT];
-    int64_t srow[kNT];
-  #pragma unroll
-    for (int t = 0; t < kNT; ++t) {
+  const int part_of = wave % ks;
+  const int blocks = (dim + kBlock - 1) / kBlock;
+  const int steps = (blocks + ks - 1) / ks, per_chunk = chunk / (ks * kBlock);
+  const int row_bytes = chunk * 2 + 16;   // (16 rows' pieces fall on different banks)
+  const int64_t cb = dim / 2, sb = (int64_t)(dim / GROUP) * (MODE == kF32Each ? 4 : 2);
+
+  // loads run ahead of the sums: (l_item, l_step), with the lane's table rows
+  const uint8_t *row[NT], *srow[NT];
+  int64_t l_item = blockIdx.x;
+  int l_step = 0;
+  auto point = [&]() {
+    const int64_t rb = l_item % row_blocks;
+    const int64_t n0 = (rb * (4 / ks) + wave / ks) * (16 * NT);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      // (rows past the last are stood in for by the last: their sums are not stored)
       int64_t r = n0 + t * 16 + i16;
-      if (r >= rows) r = rows - 1;
+      r = r < rows ? r : rows - 1;
       row[t] = codes + r * cb;
-      srow[t] = r * groups;
+      srow[t] = scales + r * sb;
     }
-    const uint8_t *xrow[MT];
-    bool xin[MT];
-  #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      const int64_t r = m0 + m * 16 + i16;
-      xin[m] = r < n_x;
-      xrow[m] = x + (xin[m] ? r : 0) * dim * XB;
+  };
+  using Blk = Block<GROUP, NT, MODE>;
+  auto load = [&](Blk &blk) {
+    const int kb = l_step * ks + part_of;
+    blk.load(kb < blocks ? kb : blocks - 1, dim, row, srow, p);
+    if (++l_step == steps) {
+      l_step = 0;
+      if (l_item + gridDim.x < items) l_item += gridDim.x;   // (past the end: once more)
+      point();
     }
-    for (int kb = k0; kb < k1; ++kb) {
-      const int c0 = kb * 128;
-      uint32_t w[kNT][4];
-      float sc[kNT][NG];
-  #pragma unroll
-      for (int t = 0; t < kNT; ++t) {
-        u32x4v_t v = {0u, 0u, 0u, 0u};
-        if (c0 + p * 32 < dim) v = *(const u32x4v_t *)(row[t] + (c0 + p * 32) / 2);
-  #pragma unroll
-        for (int j = 0; j < 4; ++j) w[t][j] = v[j];
-  #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          const int64_t at = srow[t] + c0 / GROUP + g;
-          sc[t][g] = c0 + g * GROUP >= dim ? 0.0f
-                     : scale_bf16 ? bf16_to_f32(((const uint16_t *)scales)[at])
-                                  : ((const float *)scales)[at];
-        }
+  };
+
+  f32x4_t tot[NT][MT];
+  int64_t item = blockIdx.x;
+  int step = 0;
+  int64_t mb = 0, rb = 0, m0 = 0;
+  int mrows = 0, part_bytes = 0;
+  int64_t staged = -1;   // block of rows of x that is staged as a whole
+  auto add = [&](Blk &blk) {
+    if (step == 0) {
+      mb = item / row_blocks;
+      rb = item - mb * row_blocks;
+      m0 = mb * (16 * MT);
+      mrows = (int)(n_x - m0 < 16 * MT ? n_x - m0 : 16 * MT);
+      part_bytes = mrows * row_bytes;
+    }
+    const int in_chunk = step % per_chunk;
+    if (in_chunk == 0 && staged != mb) {
+      const int left = (blocks - step * ks) * kBlock;
+      __syncthreads();   // (the readers of what was staged are done)
+      stage_x<XT>(x, m0, mrows, dim, step * ks * kBlock, left < chunk ? left : chunk, row_bytes,
+                  part_bytes, xs);
+      __syncthreads();
+      if (per_chunk >= steps) staged = mb;
+    }
+    if (step == 0) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) tot[t][m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    const int kb = step * ks + part_of;
+    if (kb < blocks) {
+      const uint8_t *xc[MT];
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const int r = m * 16 + i16;
+        xc[m] = xs + (r < mrows ? r : mrows - 1) * row_bytes +
+                (in_chunk * ks + part_of) * kBlock * 2;
       }
-  #pragma unroll
-      for (int t = 0; t < kNT; ++t) exchange<GROUP>(w[t]);
-  #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        f32x4_t acc[kNT][MT];
-  #pragma unroll
-        for (int t = 0; t < kNT; ++t)
-  #pragma unroll
-          for (int m = 0; m < MT; ++m) acc[t][m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-  #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (group_of<GROUP>(j) != g) continue;
-          const int col = c0 + first_col<GROUP>(j, p);
-          bf16x8_t xa[MT][PARTS];
-  #pragma unroll
-          for (int m = 0; m < MT; ++m) load_x<XT, PARTS>(xrow[m], col, xin[m] && col < dim, xa[m]);
-  #pragma unroll
-          for (int t = 0; t < kNT; ++t) {
-            const bf16x8_t b = decode_codes(w[t][j]);
-  #pragma unroll
-            for (int m = 0; m < MT; ++m)
-  #pragma unroll
-              for (int q = PARTS - 1; q >= 0; --q)   // (small parts first)
-                acc[t][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xa[m][q], b, acc[t][m], 0, 0, 0);
-          }
-        }
-  #pragma unroll
-        for (int t = 0; t < kNT; ++t)
-  #pragma unroll
-          for (int m = 0; m < MT; ++m)
-  #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              tot[t][m][i] = __builtin_fmaf(sc[t][g], acc[t][m][i], tot[t][m][i]);
-      }
+      blk.clear(kb, dim, p);
+      blk.template add<MT, PARTS>(xc, part_bytes, p, tot);
     }
+    if (++step < steps) return;
+    step = 0;
+    item += gridDim.x;
     // (ks = 4: waves 1-3 into wave 0; ks = 2: waves 1 and 3 into 0 and 2)
     if (ks > 1) {
+      __syncthreads();   // (the last item's sums are read)
       if (part_of > 0) {
-  #pragma unroll
-        for (int t = 0; t < kNT; ++t)
-  #pragma unroll
-          for (int m = 0; m < MT; ++m) joined[wave - 1][t * MT + m][lane] = tot[t][m];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+            joined[((wave - 1) * NT * MT + t * MT + m) * 64 + lane] = tot[t][m];
       }
       __syncthreads();
-      for (int q = 1; q < ks && part_of == 0; ++q) {
-  #pragma unroll
-        for (int t = 0; t < kNT; ++t)
-  #pragma unroll
+      if (part_of > 0) return;
+      for (int q = 1; q < ks; ++q) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
           for (int m = 0; m < MT; ++m) {
-            const f32x4_t o = joined[wave + q - 1][t * MT + m][lane];
-  #pragma unroll
+            const f32x4_t o = joined[((wave + q - 1) * NT * MT + t * MT + m) * 64 + lane];
+#pragma unroll
             for (int i = 0; i < 4; ++i) tot[t][m][i] += o[i];
           }
       }
     }
-    if (part_of == 0) {
     // lane l holds table row l % 16 of a tile and rows 4 (l / 16) .. + 3 of x
-  #pragma unroll
+    const int64_t n0 = (rb * (4 / ks) + wave / ks) * (16 * NT);
+#pragma unroll
     for (int m = 0; m < MT; ++m)
-  #pragma unroll
+#pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int64_t r = m0 + m * 16 + p * 4 + i;
         if (r >= n_x) continue;
-  #pragma unroll
-        for (int t = 0; t < kNT; ++t) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
           const int64_t n = n0 + t * 16 + i16;
           if (n >= rows) continue;
           if (out_f32)
@@ -250,30 +378,61 @@ __global__ __launch_bounds__(256) void score_packed_kernel(
             ((uint16_t *)out)[r * out_stride + n] = f32_to_bf16(tot[t][m][i]);
         }
       }
-    }
-    if (ks > 1) __syncthreads();   // (the next item reuses `joined`)
+  };
+
+  Blk a, b;
+  point();
+  load(a);
+  while (item < items) {
+    load(b);
+    add(a);
+    if (item >= items) break;
+    load(a);
+    add(b);
   }
 }
 
-template <int XT, int GROUP>
+template <int XT, int GROUP, int MT, int NT>
 hipError_t launch_packed_t(const hs_row_table *t, const void *x, int64_t n_x, void *out,
                            int out_dtype, int64_t out_stride, hipStream_t st) {
-  const int mt = n_x <= 16 ? 1 : n_x <= 32 ? 2 : 4;
-  const int64_t mblocks = (n_x + 16 * mt - 1) / (16 * mt);
-  const int64_t waves = (t->rows + 63) / 64 * mblocks;
+  const int64_t mblocks = (n_x + 16 * MT - 1) / (16 * MT);
+  const int64_t waves = (t->rows + 16 * NT - 1) / (16 * NT) * mblocks;
   // the columns shared by up to four waves while there are fewer than 4,096 (16 per CU)
   int ks = 1;
-  while (ks < 4 && waves * ks < 4096 && t->dim > 128 * ks) ks *= 2;
-  const int64_t row_blocks = (t->rows + 64 * (4 / ks) - 1) / (64 * (4 / ks));
-  auto kernel = mt == 1   ? score_packed_kernel<XT, GROUP, 1>
-                : mt == 2 ? score_packed_kernel<XT, GROUP, 2>
-                          : score_packed_kernel<XT, GROUP, 4>;
+  while (ks < 4 && waves * ks < 4096 && t->dim > kBlock * ks) ks *= 2;
+  // x is staged by as many of the ks waves' steps as fit; at least one has to
+  const int mrows = (int)(n_x < 16 * MT ? n_x : 16 * MT), parts = XT == HS_F32 ? 3 : 1;
+  const int fit = (kStageMax / (mrows * parts) - 16) / (2 * kBlock);   // blocks
+  while (ks > fit) ks /= 2;
+  const int all = ((int)((t->dim + kBlock - 1) / kBlock) + ks - 1) / ks * ks;
+  const int chunk = (all < fit ? all : fit / ks * ks) * kBlock;
+  const int64_t per = 16 * NT * (4 / ks), row_blocks = (t->rows + per - 1) / per;
   const int64_t items = row_blocks * mblocks;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(items < (1 << 22) ? items : (1 << 22))), dim3(256), 0, st,
-                     (const uint8_t *)t->data, t->scale, (int)(t->scale_dtype == HS_BF16), t->rows,
-                     (int)t->dim, (const uint8_t *)x, n_x, ks, row_blocks, items, out,
+  const size_t lds = (size_t)mrows * parts * (chunk * 2 + 16) +
+                     (ks > 1 ? (size_t)3 * NT * MT * 64 * 16 : 0);
+  auto kernel = t->scale_dtype == HS_F32   ? score_packed_kernel<XT, GROUP, MT, NT, kF32Each>
+                : t->dim % kBlock == 0 ? score_packed_kernel<XT, GROUP, MT, NT, kBf16Whole>
+                                       : score_packed_kernel<XT, GROUP, MT, NT, kBf16Each>;
+  // (workgroups per CU: 24 rows x 1M x 768 took 105 us with two, 114 with four; one row
+  // x 32,000 x 4,096 18 us with three or four, 20 with two)
+  const int64_t grid = (MT == 1 ? 3 : 2) * (int64_t)persistent_grid();
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(items < grid ? items : grid)), dim3(256), lds, st,
+                     (const uint8_t *)t->data, (const uint8_t *)t->scale, t->rows, (int)t->dim,
+                     (const uint8_t *)x, n_x, ks, chunk, row_blocks, items, out,
                      (int)(out_dtype == HS_F32), out_stride);
   return hipGetLastError();
+}
+
+template <int XT, int GROUP>
+hipError_t launch_packed_g(const hs_row_table *t, const void *x, int64_t n_x, void *out,
+                           int out_dtype, int64_t out_stride, hipStream_t st) {
+  if (n_x <= 16)
+    return launch_packed_t<XT, GROUP, 1, 1>(t, x, n_x, out, out_dtype, out_stride, st);
+  // (64 rows of fp32 parts do not fit in LDS)
+  if (XT == HS_F32 || n_x <= 32)
+    return launch_packed_t<XT, GROUP, 2, 2>(t, x, n_x, out, out_dtype, out_stride, st);
+  return launch_packed_t<XT, GROUP, XT == HS_F32 ? 2 : 4, 2>(t, x, n_x, out, out_dtype,
+                                                                  out_stride, st);
 }
 
 }  // namespace
@@ -282,8 +441,8 @@ hipError_t launch_score_packed(const hs_row_table *t, const void *x, int x_dtype
                                void *out, int out_dtype, int64_t out_stride, hipStream_t st) {
   if (n_x <= 0 || t->rows <= 0) return hipSuccess;
 #define HS_PACKED(G)                                                                        \
-  (x_dtype == HS_F32 ? launch_packed_t<HS_F32, G>(t, x, n_x, out, out_dtype, out_stride, st) \
-                     : launch_packed_t<HS_BF16, G>(t, x, n_x, out, out_dtype, out_stride, st))
+  (x_dtype == HS_F32 ? launch_packed_g<HS_F32, G>(t, x, n_x, out, out_dtype, out_stride, st) \
+                     : launch_packed_g<HS_BF16, G>(t, x, n_x, out, out_dtype, out_stride, st))
   return t->group == 32 ? HS_PACKED(32) : t->group == 64 ? HS_PACKED(64) : HS_PACKED(128);
 #undef HS_PACKED
 }
