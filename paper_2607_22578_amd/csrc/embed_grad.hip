@@ -22,18 +22,23 @@ namespace {
 
 constexpr int kSmallMax = 4096;      // positions that one workgroup sorts
 constexpr int kSmallWaves = 16;
-constexpr int kSortWaves = 8;        // per tile
+constexpr int kSortWaves = 16;       // per tile
+constexpr int kRounds = 4;           // keys per lane held in registers
 constexpr int kDigitBits = 9;        // most bits of a digit
 constexpr int kDigits = 1 << kDigitBits;
-static_assert(kSortWaves * 64 == kDigits, "a thread per digit");
-constexpr int kTilesMax = 128;       // tiles of the sort
-constexpr int kTileMin = 2048;       // positions that make another tile worth it
+static_assert(kSortWaves * 64 == 2 * kDigits, "two threads per digit");
+constexpr int kTilesMax = 64;        // tiles of the sort
+constexpr int kTileMin = 4096;       // positions that make another tile worth it
 constexpr int kChunk = 64;           // sorted places of one wave, at most
+constexpr int kSpanMany = 24;        // chunks that a workgroup instead of a wave joins
 
 struct GradWs {
   uint32_t *tok[2], *pos[2];   // [n] each: sorted keys and positions
   uint32_t *hist;              // [kTilesMax][kDigits]
   uint32_t *start;             // [rows + 1]
+  uint32_t *count;             // [2]: entries of the lists
+  uint32_t *list[2];           // [chunks] each: chunks where a token over several chunks
+                               // begins, with few (0) or many (1) of them
   float *part;                 // [2 x chunks][dim]: sums of the tokens over a chunk's
                                // start (0) and end (1)
 };
@@ -63,6 +68,12 @@ size_t layout(int64_t n, int64_t rows, int64_t dim, void *base, GradWs *w) {
   at += (int64_t)kTilesMax * kDigits * 4;
   if (w) w->start = (uint32_t *)(p + at);
   at += up256((rows + 1) * 4);
+  if (w) w->count = (uint32_t *)(p + at);
+  at += 256;
+  for (int i = 0; i < 2; ++i) {
+    if (w) w->list[i] = (uint32_t *)(p + at);
+    at += up256(chunks * 4);
+  }
   if (w) w->part = (float *)(p + at);
   at += up256(chunks * 2 * dim * 4);
   return (size_t)at;
@@ -93,6 +104,24 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, bool in) {
   return m;
 }
 
+// Exclusive scan of one value per thread over the first kDigits threads of a
+// workgroup; `sums` holds kDigits / 64 words.  Every thread of the workgroup calls it.
+__device__ __forceinline__ uint32_t scan_digits(uint32_t v, uint32_t *sums) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t s = v;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t o = __shfl_up(s, d);
+    if (lane >= d) s += o;
+  }
+  if (lane == 63 && wave < kDigits / 64) sums[wave] = s;
+  __syncthreads();
+  uint32_t before = 0u;
+#pragma unroll
+  for (int w = 0; w < kDigits / 64; ++w) before += w < wave ? sums[w] : 0u;
+  return before + s - v;
+}
+
 // All passes in one workgroup, keys and positions in LDS; 16 waves, each with a
 // contiguous share and its own digit counters (made exclusive over digits and waves).
 __global__ __launch_bounds__(kSmallWaves * 64) void grad_sort_small(
@@ -100,7 +129,7 @@ __global__ __launch_bounds__(kSmallWaves * 64) void grad_sort_small(
     uint32_t *__restrict__ tok, uint32_t *__restrict__ pos) {
   __shared__ uint32_t key[2][kSmallMax], val[2][kSmallMax];
   __shared__ uint32_t cnt[kSmallWaves][kDigits];
-  __shared__ uint32_t total[kDigits];
+  __shared__ uint32_t sums[kDigits / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (int i = tid; i < n; i += kSmallWaves * 64) {
     key[0][i] = token_key(ids, is64, i, rows, pad);
@@ -116,22 +145,15 @@ __global__ __launch_bounds__(kSmallWaves * 64) void grad_sort_small(
     __syncthreads();
     for (int i = lo + lane; i < hi; i += 64) atomicAdd(&cnt[wave][(key[from][i] >> shift) & mask], 1u);
     __syncthreads();
-    // digit totals, their exclusive scan (512 digits in the first 8 waves)
+    // digit totals and their exclusive scan (512 digits in the first 8 waves)
     uint32_t mine = 0u;
     if (tid < kDigits) {
+#pragma unroll
       for (int w = 0; w < kSmallWaves; ++w) mine += cnt[w][tid];
-      total[tid] = mine;
     }
-    __syncthreads();
-    for (int d = 1; d < kDigits; d <<= 1) {
-      uint32_t add = 0u;
-      if (tid < kDigits && tid >= d) add = total[tid - d];
-      __syncthreads();
-      if (tid < kDigits) total[tid] += add;
-      __syncthreads();
-    }
+    uint32_t base = scan_digits(mine, sums);
     if (tid < kDigits) {
-      uint32_t base = total[tid] - mine;
+#pragma unroll
       for (int w = 0; w < kSmallWaves; ++w) {
         const uint32_t c = cnt[w][tid];
         cnt[w][tid] = base;
@@ -170,7 +192,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void grad_count(
     const void *__restrict__ ids, int is64, const uint32_t *__restrict__ tok, int64_t n,
     int64_t tile, int64_t rows, int64_t pad, int bits, int shift, uint32_t *__restrict__ hist) {
   __shared__ uint32_t cnt[kDigits];
-  cnt[threadIdx.x] = 0u;
+  if (threadIdx.x < kDigits) cnt[threadIdx.x] = 0u;
   __syncthreads();
   const int64_t lo = (int64_t)blockIdx.x * tile, hi = lo + tile < n ? lo + tile : n;
   const uint32_t mask = (1u << bits) - 1u;
@@ -179,11 +201,14 @@ __global__ __launch_bounds__(kSortWaves * 64) void grad_count(
     atomicAdd(&cnt[(k >> shift) & mask], 1u);
   }
   __syncthreads();
-  hist[(int64_t)blockIdx.x * kDigits + threadIdx.x] = cnt[threadIdx.x];
+  if (threadIdx.x < kDigits)
+    hist[(int64_t)blockIdx.x * kDigits + threadIdx.x] = cnt[threadIdx.x];
 }
 
 // Stable scatter of one tile.  The tile's first place of each digit comes straight
-// from the counts of all tiles (at most 128 reads per digit and workgroup).
+// from the counts of all tiles: two threads per digit, 32 reads each at most, all in
+// flight at once (with 128 tiles and 8 in flight they were most of the launch: 16 us for
+// 262,144 positions).
 template <bool FIRST>
 __global__ __launch_bounds__(kSortWaves * 64) void grad_scatter(
     const void *__restrict__ ids, int is64, const uint32_t *__restrict__ tok,
@@ -191,65 +216,91 @@ __global__ __launch_bounds__(kSortWaves * 64) void grad_scatter(
     int64_t pad, int bits, int shift, const uint32_t *__restrict__ hist,
     uint32_t *__restrict__ tok_out, uint32_t *__restrict__ pos_out) {
   __shared__ uint32_t cnt[kSortWaves][kDigits];
-  __shared__ uint32_t total[kDigits];
+  __shared__ uint32_t other[2][kDigits];
+  __shared__ uint32_t sums[kDigits / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const uint32_t mask = (1u << bits) - 1u;
   const int64_t lo = (int64_t)blockIdx.x * tile, hi = lo + tile < n ? lo + tile : n;
   const int64_t share = tile / kSortWaves;   // (a multiple of 64)
   const int64_t wlo = lo + wave * share < hi ? lo + wave * share : hi;
   const int64_t whi = wlo + share < hi ? wlo + share : hi;
-  for (int w = 0; w < kSortWaves; ++w) cnt[w][tid] = 0u;
+  for (int i = tid; i < kSortWaves * kDigits; i += kSortWaves * 64) (&cnt[0][0])[i] = 0u;
   __syncthreads();
-  for (int64_t i = wlo + lane; i < whi; i += 64) {
+  // the wave's first kRounds x 64 keys stay in registers (all of them, up to 262,144
+  // positions): their loads are in flight together, and with those of the counts
+  uint32_t key[kRounds], val[kRounds];
+  auto fetch = [&](int64_t i0) {
+#pragma unroll
+    for (int u = 0; u < kRounds; ++u) {
+      const int64_t i = i0 + u * 64 + lane;
+      key[u] = val[u] = 0u;
+      if (i < whi) {
+        key[u] = FIRST ? token_key(ids, is64, i, rows, pad) : tok[i];
+        val[u] = FIRST ? (uint32_t)i : pos[i];
+      }
+    }
+  };
+  fetch(wlo);
+#pragma unroll
+  for (int u = 0; u < kRounds; ++u)
+    if (wlo + u * 64 + lane < whi) atomicAdd(&cnt[wave][(key[u] >> shift) & mask], 1u);
+  for (int64_t i = wlo + kRounds * 64 + lane; i < whi; i += 64) {
     const uint32_t k = FIRST ? token_key(ids, is64, i, rows, pad) : tok[i];
     atomicAdd(&cnt[wave][(k >> shift) & mask], 1u);
   }
+  const int digit = tid & (kDigits - 1), half = tid / kDigits;
   uint32_t before = 0u, all = 0u;
-#pragma unroll 8
-  for (int t = 0; t < tiles; ++t) {
-    const uint32_t c = hist[(int64_t)t * kDigits + tid];
-    if (t < (int)blockIdx.x) before += c;
+#pragma unroll
+  for (int i = 0; i < kTilesMax / 2; ++i) {
+    const int t = 2 * i + half;
+    const uint32_t c = t < tiles ? hist[t * kDigits + digit] : 0u;
+    before += t < (int)blockIdx.x ? c : 0u;
     all += c;
   }
-  total[tid] = all;
-  __syncthreads();
-  for (int d = 1; d < kDigits; d <<= 1) {
-    const uint32_t add = tid >= d ? total[tid - d] : 0u;
-    __syncthreads();
-    total[tid] += add;
-    __syncthreads();
-  }
-  uint32_t base = total[tid] - all + before;
-  for (int w = 0; w < kSortWaves; ++w) {
-    const uint32_t c = cnt[w][tid];
-    cnt[w][tid] = base;
-    base += c;
+  if (half == 1) {
+    other[0][digit] = before;
+    other[1][digit] = all;
   }
   __syncthreads();
-  for (int64_t i0 = wlo; i0 < whi; i0 += 64) {
-    const int64_t i = i0 + lane;
-    const bool in = i < whi;
-    uint32_t k = 0u, v = 0u;
-    if (in) {
-      k = FIRST ? token_key(ids, is64, i, rows, pad) : tok[i];
-      v = FIRST ? (uint32_t)i : pos[i];
+  if (half == 0) {
+    before += other[0][digit];
+    all += other[1][digit];
+  }
+  uint32_t base = scan_digits(half == 0 ? all : 0u, sums) + before;
+  if (half == 0) {
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      const uint32_t c = cnt[w][digit];
+      cnt[w][digit] = base;
+      base += c;
     }
-    const uint32_t d = (k >> shift) & mask;
-    const uint64_t same = same_digit(d, bits, in);
-    if (in) {
-      const uint32_t at = cnt[wave][d] + (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
-      tok_out[at] = k;
-      pos_out[at] = v;
+  }
+  __syncthreads();
+  for (int64_t i0 = wlo; i0 < whi; i0 += kRounds * 64) {
+    if (i0 > wlo) fetch(i0);
+#pragma unroll
+    for (int u = 0; u < kRounds; ++u) {
+      const bool in = i0 + u * 64 + lane < whi;
+      const uint32_t d = (key[u] >> shift) & mask;
+      const uint64_t same = same_digit(d, bits, in);
+      if (in) {
+        const uint32_t at = cnt[wave][d] + (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
+        tok_out[at] = key[u];
+        pos_out[at] = val[u];
+      }
+      wave_fence();
+      if (in && (same >> lane) == 1ull) cnt[wave][d] += (uint32_t)__popcll(same);
+      wave_fence();
     }
-    wave_fence();
-    if (in && (same >> lane) == 1ull) cnt[wave][d] += (uint32_t)__popcll(same);
-    wave_fence();
   }
 }
 
-// start[v] for v <= rows: the first sorted place whose token is v or above.
+// start[v] for v <= rows: the first sorted place whose token is v or above.  Also
+// empties the lists.
 __global__ __launch_bounds__(256) void grad_starts(const uint32_t *__restrict__ tok, int64_t n,
-                                                   int64_t rows, uint32_t *__restrict__ start) {
+                                                   int64_t rows, uint32_t *__restrict__ start,
+                                                   uint32_t *__restrict__ count) {
+  if (blockIdx.x == 0 && threadIdx.x < 2) count[threadIdx.x] = 0u;
   for (int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x; v <= rows;
        v += (int64_t)gridDim.x * 256) {
     int64_t a = 0, b = n;
@@ -352,7 +403,8 @@ __global__ __launch_bounds__(256) void grad_sums(
     const uint8_t *__restrict__ grad, const uint32_t *__restrict__ tok,
     const uint32_t *__restrict__ pos, const uint32_t *__restrict__ start, int64_t n, int64_t rows,
     int dim, int places, int64_t chunks, int slices, int64_t sum_blocks, float scale, int add,
-    float *__restrict__ part, uint8_t *__restrict__ table) {
+    float *__restrict__ part, uint32_t *__restrict__ count, uint32_t *__restrict__ few,
+    uint32_t *__restrict__ many, uint8_t *__restrict__ table) {
   using S = Slice<DT, WIDE>;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if ((int64_t)blockIdx.x >= sum_blocks) {
@@ -420,6 +472,11 @@ __global__ __launch_bounds__(256) void grad_sums(
     S::part(part + (c * 2) * dim, col0, lane, dim, acc);
   } else if (cur == next) {
     S::part(part + (c * 2 + 1) * dim, col0, lane, dim, acc);
+    if (col0 == 0 && lane == 0) {
+      const int64_t span = ((int64_t)start[cur + 1] - 1) / places - c;
+      const int l = span >= kSpanMany ? 1 : 0;
+      (l ? many : few)[atomicAdd(&count[l], 1u)] = (uint32_t)c;
+    }
   } else {
 #pragma unroll
     for (int j = 0; j < S::V; ++j) acc[j] *= scale;
@@ -427,43 +484,81 @@ __global__ __launch_bounds__(256) void grad_sums(
   }
 }
 
-// Tokens over several chunks: the workgroup of the chunk where the token begins adds
-// that chunk's partial sum and those of the following chunks, 64 columns at a time,
-// four contiguous shares of the chunks by four waves, joined in order.
+// Tokens over several chunks: the sum at the end of the chunk where the token begins
+// and those at the start of the following ones, 256 columns at a time.  A wave joins
+// a few chunks, in order; a workgroup many, in four contiguous shares whose sums are
+// added in order.
+template <int OT>
+__device__ __forceinline__ void join_write(uint8_t *table, int64_t t, int col, int dim,
+                                           float scale, int add, const float *v) {
+  uint8_t *row = table + t * dim * (OT == HS_F32 ? 4 : 2);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int c = col + j * 64;
+    if (c < dim) {
+      const float x = v[j] * scale;
+      store_col<OT>(row, c, add ? x + load_col<OT>(row, c) : x);
+    }
+  }
+}
+
+__device__ __forceinline__ void join_sum(const float *part, int64_t a, int64_t b, int col, int dim,
+                                         float *v) {
+#pragma unroll 4
+  for (int64_t k = a; k < b; ++k) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int c = col + j * 64;
+      v[j] += part[k * 2 * dim + (c < dim ? c : 0)];
+    }
+  }
+}
+
 template <int OT>
 __global__ __launch_bounds__(256) void grad_join(
-    const uint32_t *__restrict__ tok, const uint32_t *__restrict__ start, int64_t n, int64_t rows,
-    int dim, int places, int col_blocks, int64_t tasks, float scale, int add,
-    const float *__restrict__ part,
-    uint8_t *__restrict__ table) {
-  __shared__ float sums[4][64];
+    const uint32_t *__restrict__ tok, const uint32_t *__restrict__ start, int dim, int places,
+    int col_blocks, float scale, int add, const uint32_t *__restrict__ count,
+    const uint32_t *__restrict__ few, const uint32_t *__restrict__ many,
+    const float *__restrict__ part, uint8_t *__restrict__ table) {
+  __shared__ float sums[4][256];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int64_t task = blockIdx.x; task < tasks; task += gridDim.x) {
-    const int64_t c = task / col_blocks;
-    const int col = (int)(task - c * col_blocks) * 64 + lane;
-    const int64_t end = (c + 1) * places;   // < n: the last chunk has no task
-    const uint32_t t = tok[end - 1];
-    if (t == (uint32_t)rows || tok[end] != t) continue;
-    const int64_t first = start[t], last = (int64_t)start[t + 1] - 1;
-    if (first < c * places) continue;   // began earlier: that chunk's task joins it
-    // chunks c + 1 .. c1 hold the token's other sums
-    const int64_t c1 = last / places, count = c1 - c, share = (count + 3) / 4;
+  const int64_t n_many = (int64_t)count[1] * col_blocks, n_few = (int64_t)count[0] * col_blocks;
+  for (int64_t task = blockIdx.x; task < n_many; task += gridDim.x) {
+    const int64_t e = task / col_blocks, c = many[e];
+    const int col = (int)(task - e * col_blocks) * 256 + lane;
+    const uint32_t t = tok[(c + 1) * places - 1];
+    const int64_t c1 = ((int64_t)start[t + 1] - 1) / places;   // its last chunk
+    const int64_t share = (c1 - c + 3) / 4;
     const int64_t a = c + 1 + wave * share, b = a + share < c1 + 1 ? a + share : c1 + 1;
-    float acc = 0.0f;
-    if (col < dim) {
-      if (wave == 0) acc = part[(c * 2 + 1) * dim + col];
-#pragma unroll 8
-      for (int64_t k = a; k < b; ++k) acc += part[k * 2 * dim + col];
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (wave == 0) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = col + j * 64 < dim ? part[(c * 2 + 1) * dim + col + j * 64] : 0.0f;
     }
-    sums[wave][lane] = acc;
+    join_sum(part, a, b, col, dim, v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sums[wave][j * 64 + lane] = v[j];
     __syncthreads();
-    if (wave == 0 && col < dim) {
-      float v = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
-      v *= scale;
-      uint8_t *row = table + (int64_t)t * dim * (OT == HS_F32 ? 4 : 2);
-      store_col<OT>(row, col, add ? v + load_col<OT>(row, col) : v);
+    if (wave == 0) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = j * 64 + lane;
+        v[j] = ((sums[0][i] + sums[1][i]) + sums[2][i]) + sums[3][i];
+      }
+      join_write<OT>(table, t, col, dim, scale, add, v);
     }
     __syncthreads();
+  }
+  for (int64_t task = (int64_t)blockIdx.x * 4 + wave; task < n_few; task += (int64_t)gridDim.x * 4) {
+    const int64_t e = task / col_blocks, c = few[e];
+    const int col = (int)(task - e * col_blocks) * 256 + lane;
+    const uint32_t t = tok[(c + 1) * places - 1];
+    const int64_t c1 = ((int64_t)start[t + 1] - 1) / places;
+    float v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = col + j * 64 < dim ? part[(c * 2 + 1) * dim + col + j * 64] : 0.0f;
+    join_sum(part, c + 1, c1 + 1, col, dim, v);
+    join_write<OT>(table, t, col, dim, scale, add, v);
   }
 }
 
@@ -481,13 +576,15 @@ hipError_t launch_sums(const GradWs &w, int side, const void *grad, int64_t n, i
   hipLaunchKernelGGL((wide ? grad_sums<DT, OT, true> : grad_sums<DT, OT, false>),
                      dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, st,
                      (const uint8_t *)grad, w.tok[side], w.pos[side], w.start, n, rows, (int)dim,
-                     places, chunks, slices, sum_blocks, scale, add, w.part, (uint8_t *)table);
-  const int col_blocks = (int)((dim + 63) / 64);
-  const int64_t tasks = (chunks - 1) * col_blocks;
-  if (tasks > 0)
-    hipLaunchKernelGGL(grad_join<OT>, dim3((unsigned)(tasks < 65536 ? tasks : 65536)), dim3(256),
-                       0, st, w.tok[side], w.start, n, rows, (int)dim, places, col_blocks, tasks,
-                       scale, add, w.part, (uint8_t *)table);
+                     places, chunks, slices, sum_blocks, scale, add, w.part, w.count, w.list[0],
+                     w.list[1], (uint8_t *)table);
+  if (chunks > 1) {
+    const int col_blocks = (int)((dim + 255) / 256);
+    const int64_t tasks = ((chunks - 1) * col_blocks + 3) / 4;   // (as many at most, in waves)
+    hipLaunchKernelGGL(grad_join<OT>, dim3((unsigned)(tasks < 1024 ? tasks : 1024)), dim3(256), 0,
+                       st, w.tok[side], w.start, (int)dim, places, col_blocks, scale, add, w.count,
+                       w.list[0], w.list[1], w.part, (uint8_t *)table);
+  }
   return hipGetLastError();
 }
 
@@ -538,7 +635,7 @@ hipError_t launch_embed_grad(const void *grad, int grad_dtype, const void *ids, 
   int64_t blocks = (rows + 256) / 256;
   if (blocks > 4096) blocks = 4096;
   hipLaunchKernelGGL(grad_starts, dim3((unsigned)blocks), dim3(256), 0, st, w.tok[side], n, rows,
-                     w.start);
+                     w.start, w.count);
   if (grad_dtype == HS_F32)
     return table_dtype == HS_F32
                ? launch_sums<HS_F32, HS_F32>(w, side, grad, n, rows, dim, scale, add, table, st)
