@@ -247,17 +247,4 @@ hipError_t launch_topk_merge(const void *part, int64_t n_unique, const int64_t *
   return hipGetLastError();
 }
 
-// The merge alone, for sorted slice lists [n_rows x S x k] of other kernels; S as
-// make_split gives it for tiles of one row and nc columns.
-hipError_t launch_lists_merge(const void *part, int64_t n_rows, int64_t n_cols, int k, int nc,
-                              int64_t smax, int grid, float *out_s, int32_t *out_i,
-                              hipStream_t st) {
-  const int64_t blocks = n_rows < 2 * (int64_t)grid ? n_rows : 2 * (int64_t)grid;
-  hipLaunchKernelGGL(topk_merge_kernel<false>, dim3((unsigned)blocks), dim3(kMergeThreads), 0, st,
-                     (const uint64_t *)part, (const uint32_t *)nullptr, n_rows,
-                     (const int64_t *)nullptr, n_rows, n_cols, k, 1, nc, smax, 0u, grid, out_s,
-                     out_i);
-  return hipGetLastError();
-}
-
 }  // namespace hs

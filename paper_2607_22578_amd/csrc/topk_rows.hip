@@ -1,12 +1,16 @@
 // The k best columns of materialised rows of scores.
 //
-// Phase 1: work items are (row, slice of columns) as in the score kernels
-// (make_split).  A workgroup streams its slice in tiles and keeps, in LDS, the keys
-// (ordered score, ~column) that may be among the slice's k best: those above a
-// bound that starts as the k-th largest of the threads' maxima of the first tile and
-// is made exact whenever the buffer has filled.  It leaves the slice's sorted k best.
-// Phase 2: the merge of the score step (topk_merge_kernel).  With one slice per row
-// phase 1 writes the results itself.
+// Phase 1 (rows above 32,768 columns): the largest score of every strip, a thread's
+// columns of a tile; nothing but a stream over the scores.
+// Phase 2: a workgroup per row.  A score that k of the strips' maxima (or of its
+// threads' maxima over them) reach is a lower bound of the k-th best, and a close one
+// while there are many more strips than k; only the strips that reach it are read
+// again, and the few columns in them that reach it are ranked by counting.  Shorter
+// rows are their own maxima.  Where too many columns reach the bound (equal scores) the
+// k-th best score is found bit by bit, and the columns that have it are taken in
+// ascending order.
+// Loops are short on purpose: with one workgroup on a CU, fetching straight-line code
+// took longer than reading the maxima twice (17 against 11 us, 1 x 32,000, k = 50).
 // Floor: the scores, read once.
 #include "rows.h"
 
@@ -14,221 +18,343 @@ namespace hs {
 
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kPer = 8;                      // columns per thread and tile
-constexpr int kTile = kThreads * kPer;
-constexpr int kKeep = 2048;                  // keys kept from one tile to the next, at most
-constexpr int kBuf = kKeep + kTile;
-constexpr int kPerBuf = kBuf / kThreads;
-constexpr int kListMax = 8192;               // keys of one row's lists (the merge's LDS)
+constexpr int kRowCols = 32768;    // longest row done without strips
+constexpr int kStripsMax = 16384;   // strips of a row
+constexpr int kStripThreads = 256;
+constexpr int kLeastReads = 4;     // accesses of a strip, at least
 
-struct Shared {
-  uint64_t buf[kBuf];
-  uint32_t maxima[kThreads];
-  uint32_t sums[2][kThreads / 64];
-  uint32_t bound;
-  int count;
-};
+// Ordered score; 0 (below every real one) for -inf and NaN, which are never taken.
+__device__ __forceinline__ uint32_t taken_score(float v) {
+  return v > -__builtin_inff() ? ord_score(v) : 0u;
+}
 
-// The k-th largest of the 512 maxima (ordered scores), found by wave 0 bit by bit
-// from the top: eight values a lane, a ballot for each.
-__device__ __forceinline__ uint32_t kth_maximum(const uint32_t *maxima, int lane, int k) {
-  uint32_t v[kThreads / 64];
+template <int DT, bool WIDE>
+constexpr __host__ __device__ int access_cols() {
+  return WIDE ? (DT == HS_F32 ? 4 : 8) : 1;
+}
+
+// f(score, column) for the columns of U accesses (C columns from col[u] on, which may end
+// past the row or lie past it).  All loads are in flight together: those outside are
+// made at the row's start instead.  (Rows have at least C columns.)
+template <int DT, bool WIDE, int U, class F>
+__device__ __forceinline__ void visit(const uint8_t *row, const int64_t *col, int64_t n_cols,
+                                      F f) {
+  constexpr int C = access_cols<DT, WIDE>();
+  if constexpr (WIDE) {
+    RawCols<DT, WIDE ? C : 4> raw[U];
 #pragma unroll
-  for (int i = 0; i < kThreads / 64; ++i) v[i] = maxima[i * 64 + lane];
+    for (int u = 0; u < U; ++u) raw[u].load(row, col[u] + C <= n_cols ? col[u] : 0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (col[u] + C <= n_cols) {
+        float v[C];
+        raw[u].decode(v);
+#pragma unroll
+        for (int j = 0; j < C; ++j) f(v[j], col[u] + j);
+      } else {
+#pragma unroll 1
+        for (int64_t c = col[u]; c < n_cols; ++c) f(load_col<DT>(row, c), c);
+      }
+    }
+  } else {
+    float v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = load_col<DT>(row, col[u] < n_cols ? col[u] : 0);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (col[u] < n_cols) f(v[u], col[u]);
+  }
+}
+
+// ---------------------------------------------------------------- strips
+//
+// Strip j = 256 t + i of a row: accesses i, i + 256, ... (`reads` of them) of tile t.
+// 24 rows x 1M fp32: 22 us, 4.3 TB/s.
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(kStripThreads) void strip_maxima_kernel(
+    const uint8_t *__restrict__ scores, int64_t stride, int64_t n_cols, int reads, int64_t tiles,
+    int64_t items, uint32_t *__restrict__ maxima) {
+  constexpr int ES = DT == HS_F32 ? 4 : 2, C = access_cols<DT, WIDE>(), U = kLeastReads;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int64_t r = item / tiles, t = item - r * tiles;
+    const uint8_t *row = scores + r * stride * ES;
+    const int64_t c0 = t * kStripThreads * C * reads + threadIdx.x * C;
+    float mx = -__builtin_inff();
+    for (int i = 0; i < reads; i += U) {
+      int64_t col[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) col[u] = c0 + (int64_t)(i + u) * kStripThreads * C;
+      visit<DT, WIDE, U>(row, col, n_cols,
+                         [&](float v, int64_t) { mx = fmaxf(mx, v); });   // (a NaN loses)
+    }
+    maxima[item * kStripThreads + threadIdx.x] = taken_score(mx);
+  }
+}
+
+// ---------------------------------------------------------------- selection
+
+// A score that at least k of 64 E values reach, found by one wave bit by bit from the
+// top until hardly more than k do.
+template <int E>
+__device__ __forceinline__ uint32_t bound_of(const uint32_t *v, int k) {
   uint32_t t = 0u;
+#pragma unroll 1
   for (int b = 31; b >= 0; --b) {
     const uint32_t c = t | (1u << b);
     int n = 0;
 #pragma unroll
-    for (int i = 0; i < kThreads / 64; ++i) n += __popcll(__builtin_amdgcn_ballot_w64(v[i] >= c));
-    if (n >= k) t = c;
-    if (n == k) break;
+    for (int i = 0; i < E; ++i) n += __popcll(__builtin_amdgcn_ballot_w64(v[i] >= c));
+    if (n >= k) {
+      t = c;
+      if (n <= k + k / 8) break;
+    }
   }
   return t;
 }
 
-// Cuts the buffer's m > k keys to the k largest (in any order); returns the k-th.
-__device__ uint64_t cut(Shared &s, int m, int k) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  uint64_t key[kPerBuf];
+// The same for T maxima in LDS, combined first to the fewest that are 3 k or more: fewer
+// ballots, and the bound still lets 1.2 k scores through, hardly more.
+template <int T>
+__device__ __forceinline__ uint32_t bound_of_maxima(const uint32_t *maxima, int lane, int k) {
+  constexpr int E = T / 64;
+  uint32_t v[E];
 #pragma unroll
-  for (int i = 0; i < kPerBuf; ++i) {
-    const int j = i * kThreads + tid;
-    key[i] = j < m ? s.buf[j] : 0ull;
-  }
-  uint64_t t = 0ull;
-  for (int b = 63; b >= 0; --b) {
-    const uint64_t c = t | (1ull << b);
-    uint32_t n = 0u;
+  for (int i = 0; i < E; ++i) v[i] = maxima[i * 64 + lane];
+  if (E >= 16 && 3 * k > T / 2) return bound_of<E>(v, k);
 #pragma unroll
-    for (int i = 0; i < kPerBuf; ++i) n += __popcll(__builtin_amdgcn_ballot_w64(key[i] >= c));
-    if (lane == 0) s.sums[b & 1][wave] = n;
+  for (int i = 0; i < E / 2; ++i) v[i] = v[i] > v[i + E / 2] ? v[i] : v[i + E / 2];
+  if (3 * k > T / 4) return bound_of<E / 2>(v, k);
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i) v[i] = v[i] > v[i + E / 4] ? v[i] : v[i + E / 4];
+  return bound_of<E / 4>(v, k);
+}
+
+// Workgroups of T threads, a row at a time.  STRIPS: the maxima of n_strips strips
+// (a multiple of 256) of 2^reads_log accesses each are in `maxima`.
+template <int DT, bool WIDE, bool STRIPS, int T>
+__global__ __launch_bounds__(T) void select_rows_kernel(
+    const uint8_t *__restrict__ scores, int64_t stride, int64_t n_rows, int64_t n_cols, int k,
+    const uint32_t *__restrict__ maxima, int n_strips, int reads_log, float *__restrict__ out_s,
+    int32_t *__restrict__ out_i) {
+  constexpr int ES = DT == HS_F32 ? 4 : 2, C = access_cols<DT, WIDE>();
+  constexpr int CAP = T * 6;   // (at least k - 1 keys and the 4 T columns of a tie chunk)
+  __shared__ uint64_t buf[CAP];
+  __shared__ uint32_t group[T];
+  __shared__ uint16_t strip[STRIPS ? kStripsMax : 1];
+  __shared__ uint32_t bound;
+  __shared__ int count, strips;
+  const int tid = threadIdx.x, lane = tid & 63;
+  for (int64_t r = blockIdx.x; r < n_rows; r += gridDim.x) {
+    const uint8_t *row = scores + r * stride * ES;
+    const uint32_t *row_max = maxima + r * n_strips;
+    // f(ordered score, index) for the thread's maxima: those of strips, or the scores
+    auto each_max = [&](auto f) {
+      if constexpr (STRIPS) {
+#pragma unroll 4
+        for (int i = tid; i < n_strips / 4; i += T) {
+          const uint4 m = ((const uint4 *)row_max)[i];
+          f(m.x, 4 * i);
+          f(m.y, 4 * i + 1);
+          f(m.z, 4 * i + 2);
+          f(m.w, 4 * i + 3);
+        }
+      } else {
+        for (int i = tid * C; i < n_cols; i += 4 * T * C) {
+          const int64_t col[4] = {i, i + T * C, i + 2 * T * C, i + 3 * T * C};
+          visit<DT, WIDE, 4>(row, col, n_cols,
+                             [&](float v, int64_t c) { f(taken_score(v), (int)c); });
+        }
+      }
+    };
+    // f(ordered score, column) for the thread's columns that may reach the bound
+    auto each_col = [&](auto f) {
+      if constexpr (STRIPS) {
+        const int all = strips << reads_log;
+        for (int i0 = tid; i0 < all; i0 += 4 * T) {
+          int64_t col[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int i = i0 + u * T;
+            const int j = strip[i < all ? i >> reads_log : 0];
+            const int64_t at = ((int64_t)(j / kStripThreads) << reads_log) +
+                               (i & ((1 << reads_log) - 1));
+            col[u] = i < all ? (at * kStripThreads + j % kStripThreads) * C : n_cols;
+          }
+          visit<DT, WIDE, 4>(row, col, n_cols,
+                             [&](float v, int64_t c) { f(taken_score(v), (uint32_t)c); });
+        }
+      } else {
+        each_max([&](uint32_t o, int c) { f(o, (uint32_t)c); });
+      }
+    };
+    // How many of the scores that `each` visits pass f; `count` is left at that.
+    auto tally = [&](auto each, auto f) {
+      __syncthreads();
+      if (tid == 0) count = 0;
+      __syncthreads();
+      int n = 0;
+      each([&](uint32_t o, uint32_t) { n += f(o) ? 1 : 0; });
+      if (n) atomicAdd(&count, n);
+      __syncthreads();
+      return count;
+    };
+    uint32_t b = 0u;
+    if (k <= T / 4) {
+      uint32_t mx = 0u;
+      each_max([&](uint32_t o, int) { mx = o > mx ? o : mx; });
+      group[tid] = mx;
+      __syncthreads();
+      if (tid < 64) {
+        const uint32_t t = bound_of_maxima<T>(group, lane, k);
+        if (lane == 0) bound = t;
+      }
+      __syncthreads();
+      b = bound;
+    } else {
+#pragma unroll 1
+      for (int i = 31; i >= 0; --i) {
+        const uint32_t c = b | (1u << i);
+        const int n = tally(each_max, [&](uint32_t o) { return o >= c; });
+        if (n >= k) {
+          b = c;
+          if (n <= k + k / 8) break;   // (the same for every thread)
+        }
+      }
+    }
+    b = b > 0u ? b : 1u;
     __syncthreads();
-    n = 0u;
+    if (tid == 0) count = strips = 0;
+    __syncthreads();
+    if constexpr (STRIPS) {
+      each_max([&](uint32_t o, int j) {
+        if (o >= b) strip[atomicAdd(&strips, 1)] = (uint16_t)j;
+      });
+      __syncthreads();
+    }
+    each_col([&](uint32_t o, uint32_t c) {
+      if (o >= b) {
+        const int at = atomicAdd(&count, 1);
+        if (at < CAP) buf[at] = (uint64_t)o << 32 | ~c;
+      }
+    });
+    __syncthreads();
+    int m = count;
+    if (m > CAP) {
+      // t: the k-th best score; often the bound itself (equal scores)
+      uint32_t t = b;
+      int above = tally(each_col, [&](uint32_t o) { return o > t; });
+      if (above >= k) {
+        t = 0u;
+#pragma unroll 1
+        for (int i = 31; i >= 0; --i) {
+          const uint32_t c = t | (1u << i);
+          if (tally(each_col, [&](uint32_t o) { return o >= c; }) >= k) t = c;
+        }
+      }
+      __syncthreads();
+      if (tid == 0) count = 0;
+      __syncthreads();
+      each_col([&](uint32_t o, uint32_t c) {
+        if (o > t) buf[atomicAdd(&count, 1)] = (uint64_t)o << 32 | ~c;   // (below k of them)
+      });
+      __syncthreads();
+      // columns of score t, in ascending chunks, until there are k keys
+      for (int64_t c0 = 0; c0 < n_cols && count < k; c0 += 4 * T) {
+        __syncthreads();   // (everyone has seen the count)
 #pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) n += s.sums[b & 1][w];
-    if (n >= (uint32_t)k) t = c;
-    if (n == (uint32_t)k) break;   // (the same for every thread)
+        for (int u = 0; u < 4; ++u) {
+          const int64_t c = c0 + u * T + tid;
+          if (c < n_cols && taken_score(load_col<DT>(row, c)) == t)
+            buf[atomicAdd(&count, 1)] = (uint64_t)t << 32 | ~(uint32_t)c;
+        }
+        __syncthreads();
+      }
+      m = count;
+    }
+    // rank = keys above (they are distinct)
+    for (int u = tid; u < m; u += T) {
+      const uint64_t key = buf[u];
+      int rank = 0;
+#pragma unroll 8
+      for (int j = 0; j < m; ++j) rank += buf[j] > key ? 1 : 0;
+      if (rank < k) {
+        float sc;
+        int32_t c;
+        decode_key(key, sc, c);
+        out_s[r * k + rank] = sc;
+        out_i[r * k + rank] = c;
+      }
+    }
+    for (int j = m + tid; j < k; j += T) {
+      out_s[r * k + j] = -__builtin_inff();
+      out_i[r * k + j] = -1;
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  if (tid == 0) s.count = 0;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kPerBuf; ++i)
-    if (key[i] >= t) s.buf[atomicAdd(&s.count, 1)] = key[i];
-  __syncthreads();
-  return t;
+}
+
+// Accesses of a strip: a power of two, so that a row has at most kStripsMax strips.
+int strip_reads(int64_t n_cols, int cols) {
+  int reads = kLeastReads;
+  while ((n_cols + (int64_t)kStripThreads * cols * reads - 1) /
+             ((int64_t)kStripThreads * cols * reads) * kStripThreads > kStripsMax)
+    reads *= 2;
+  return reads;
+}
+
+int64_t strip_tiles(int64_t n_cols, int cols) {
+  const int64_t tile = (int64_t)kStripThreads * cols * strip_reads(n_cols, cols);
+  return (n_cols + tile - 1) / tile;
 }
 
 template <int DT, bool WIDE>
-__global__ __launch_bounds__(kThreads) void topk_rows_kernel(
-    const uint8_t *__restrict__ scores, int64_t stride, int64_t n_rows, int64_t n_cols, int k,
-    int64_t smax, int grid, uint64_t *__restrict__ part, float *__restrict__ out_s,
-    int32_t *__restrict__ out_i) {
-  __shared__ Shared s;
-  constexpr int ES = DT == HS_F32 ? 4 : 2, C = 16 / ES;
-  const Split sp = make_split(n_rows, n_cols, 1, kTile, grid, smax);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t items = n_rows * sp.S;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int64_t r = item / sp.S, slice = item - r * sp.S;
-    const int64_t t0 = slice * sp.ntiles / sp.S, t1 = (slice + 1) * sp.ntiles / sp.S;
-    const uint8_t *row = scores + r * stride * ES;
-    if (tid == 0) s.count = 0;
-    uint64_t floor_key = 0ull;   // only keys above it are kept
-    for (int64_t t = t0; t < t1; ++t) {
-      const int64_t c0 = t * kTile;
-      float v[kPer];
-      int64_t col[kPer];
-#pragma unroll
-      for (int q = 0; q < kPer; ++q) {
-        col[q] = WIDE ? c0 + (int64_t)(q / C * kThreads + tid) * C + q % C
-                      : c0 + (int64_t)q * kThreads + tid;
-      }
-      if constexpr (WIDE) {
-#pragma unroll
-        for (int q = 0; q < kPer; q += C) {
-          if (col[q] + C <= n_cols) {
-            RawCols<DT, C> raw;
-            raw.load(row, col[q]);
-            raw.decode(v + q);
-          } else {
-#pragma unroll
-            for (int j = 0; j < C; ++j)
-              v[q + j] = col[q + j] < n_cols ? load_col<DT>(row, col[q + j]) : -__builtin_inff();
-          }
-        }
-      } else {
-#pragma unroll
-        for (int q = 0; q < kPer; ++q)
-          v[q] = col[q] < n_cols ? load_col<DT>(row, col[q]) : -__builtin_inff();
-      }
-      if (t == t0 && k <= kThreads) {
-        float mx = -__builtin_inff();
-#pragma unroll
-        for (int q = 0; q < kPer; ++q) mx = fmaxf(mx, v[q]);   // (a NaN loses)
-        s.maxima[tid] = ord_score(mx);
-        __syncthreads();
-        if (wave == 0) {
-          const uint32_t b = kth_maximum(s.maxima, lane, k);
-          if (lane == 0) s.bound = b;
-        }
-      }
-      __syncthreads();
-      // (a key's low word is above 0, so keys of the bound's own score stay)
-      if (t == t0 && k <= kThreads) floor_key = (uint64_t)s.bound << 32;
-#pragma unroll
-      for (int q = 0; q < kPer; ++q) {
-        const uint64_t key = make_key(v[q], (uint32_t)col[q]);
-        const bool keep = v[q] > -__builtin_inff() && key > floor_key;
-        const uint64_t mask = __builtin_amdgcn_ballot_w64(keep);
-        if (mask) {
-          int base = 0;
-          if (lane == 0) base = atomicAdd(&s.count, __popcll(mask));
-          base = __shfl(base, 0);
-          if (keep) s.buf[base + __popcll(mask & ((1ull << lane) - 1ull))] = key;
-        }
-      }
-      __syncthreads();
-      const int m = s.count;
-      __syncthreads();
-      if (m > kKeep) floor_key = cut(s, m, k);
-    }
-    __syncthreads();
-    int m = s.count;
-    if (m > 2 * k + 256) {
-      cut(s, m, k);
-      m = k;
-    }
-    // rank = keys above (they are distinct)
-    uint64_t *list = part + item * k;
-    for (int u = tid; u < m; u += kThreads) {
-      const uint64_t key = s.buf[u];
-      int rank = 0;
-      for (int j = 0; j < m; ++j) rank += s.buf[j] > key ? 1 : 0;
-      if (rank < k) {
-        if (sp.S == 1) {
-          float sc;
-          int32_t c;
-          decode_key(key, sc, c);
-          out_s[r * k + rank] = sc;
-          out_i[r * k + rank] = c;
-        } else {
-          list[rank] = key;
-        }
-      }
-    }
-    for (int j = m + tid; j < k; j += kThreads) {
-      if (sp.S == 1) {
-        out_s[r * k + j] = -__builtin_inff();
-        out_i[r * k + j] = -1;
-      } else {
-        list[j] = 0ull;
-      }
-    }
-    __syncthreads();
+hipError_t launch_topk_t(const void *scores, int64_t stride, int64_t n_rows, int64_t n_cols, int k,
+                         void *ws, float *out_s, int32_t *out_i, hipStream_t st) {
+  const dim3 g((unsigned)(n_rows < 65536 ? n_rows : 65536));
+  const uint8_t *in = (const uint8_t *)scores;
+  if (n_cols <= kRowCols) {
+    // (256 threads do for 4,096 columns while their maxima are four times k)
+    if (n_cols <= 4096 && k <= 64)
+      hipLaunchKernelGGL((select_rows_kernel<DT, WIDE, false, 256>), g, dim3(256), 0, st, in,
+                         stride, n_rows, n_cols, k, nullptr, 0, 0, out_s, out_i);
+    else
+      hipLaunchKernelGGL((select_rows_kernel<DT, WIDE, false, 1024>), g, dim3(1024), 0, st, in,
+                         stride, n_rows, n_cols, k, nullptr, 0, 0, out_s, out_i);
+    return hipGetLastError();
   }
+  constexpr int C = access_cols<DT, WIDE>();
+  const int reads = strip_reads(n_cols, C);
+  const int64_t tiles = strip_tiles(n_cols, C), items = n_rows * tiles;
+  hipLaunchKernelGGL((strip_maxima_kernel<DT, WIDE>),
+                     dim3((unsigned)(items < (1 << 20) ? items : (1 << 20))), dim3(kStripThreads),
+                     0, st, in, stride, n_cols, reads, tiles, items, (uint32_t *)ws);
+  hipLaunchKernelGGL((select_rows_kernel<DT, WIDE, true, 1024>), g, dim3(1024), 0, st, in, stride,
+                     n_rows, n_cols, k, (const uint32_t *)ws, (int)(tiles * kStripThreads), __builtin_ctz(reads),
+                     out_s, out_i);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-int persistent_grid();
-hipError_t launch_lists_merge(const void *part, int64_t n_rows, int64_t n_cols, int k, int nc,
-                              int64_t smax, int grid, float *out_s, int32_t *out_i,
-                              hipStream_t st);
-
-static int64_t slices_max(int k) { return kListMax / k; }
-
 size_t topk_rows_workspace_bytes(int64_t n_rows, int64_t n_cols, int k) {
-  // make_split gives at most 8 rounds of a grid of at most 1,024 workgroups
-  int64_t s = (n_cols + kTile - 1) / kTile;
-  if (s > slices_max(k)) s = slices_max(k);
-  if (s > 8192 / (n_rows > 0 ? n_rows : 1)) s = 8192 / (n_rows > 0 ? n_rows : 1);
-  if (s < 1) s = 1;
-  const int64_t b = n_rows * s * k * 8;
-  return (size_t)(b < 256 ? 256 : (b + 255) & ~(int64_t)255);
+  (void)k;
+  if (n_cols <= kRowCols) return 256;
+  int64_t tiles = 0;   // the most over the access widths
+  for (int c : {1, 4, 8}) tiles = tiles > strip_tiles(n_cols, c) ? tiles : strip_tiles(n_cols, c);
+  return (size_t)(n_rows > 0 ? n_rows : 1) * (size_t)tiles * kStripThreads * 4;
 }
 
 hipError_t launch_topk_rows(const void *scores, int dtype, int64_t stride, int64_t n_rows,
                             int64_t n_cols, int k, float *out_s, int32_t *out_i, void *ws,
                             hipStream_t st) {
   if (n_rows <= 0) return hipSuccess;
-  const int grid = 2 * persistent_grid();
-  const int64_t smax = slices_max(k);
-  const Split sp = make_split(n_rows, n_cols, 1, kTile, grid, smax);
-  const int64_t items = n_rows * sp.S;
   const int es = dtype == HS_F32 ? 4 : 2;
-  const bool wide = ((uintptr_t)scores % 16) == 0 && (n_rows == 1 || stride * es % 16 == 0);
-  auto kernel = dtype == HS_F32
-                    ? (wide ? topk_rows_kernel<HS_F32, true> : topk_rows_kernel<HS_F32, false>)
-                    : (wide ? topk_rows_kernel<HS_BF16, true> : topk_rows_kernel<HS_BF16, false>);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(items < 65536 ? items : 65536)), dim3(kThreads), 0,
-                     st, (const uint8_t *)scores, stride, n_rows, n_cols, k, smax, grid,
-                     (uint64_t *)ws, out_s, out_i);
-  if (sp.S > 1)
-    return launch_lists_merge(ws, n_rows, n_cols, k, kTile, smax, grid, out_s, out_i, st);
-  return hipGetLastError();
+  const bool wide = ((uintptr_t)scores % 16) == 0 && n_cols >= 16 / es &&
+                    (n_rows == 1 || stride * es % 16 == 0);
+  auto launch = dtype == HS_F32 ? (wide ? launch_topk_t<HS_F32, true> : launch_topk_t<HS_F32, false>)
+                                : (wide ? launch_topk_t<HS_BF16, true>
+                                        : launch_topk_t<HS_BF16, false>);
+  return launch(scores, stride, n_rows, n_cols, k, ws, out_s, out_i, st);
 }
 
 }  // namespace hs
