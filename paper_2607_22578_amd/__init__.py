@@ -762,38 +762,64 @@ def merge_retrieval(keys, q_req, corpus, k: int, scale=None, workflow_offsets=No
 
 # ---------------------------------------------------------------- row tables
 
+class _Here:
+    """The context of a call on the current device and stream."""
+
+    def __enter__(self):
+        return None
+
+    def __exit__(self, *exc):
+        return False
+
+
+_HERE_CONTEXT = _Here()
+
+
 def _on(stream, device):
-    """(device context, stream) of a one-call operator: launches and new tensors belong
-    to `stream` (default: the device's current stream) whatever device and stream are
-    current."""
-    import torch
+    """(context, stream) of a one-call operator: launches and new tensors belong to
+    `stream` (a torch stream; default: the current one of the tensors' device) whatever
+    device and stream are current."""
     if device.type != "cuda":
         raise TypeError("tensors must be on a GPU")
-    if stream is None:
-        stream = torch.cuda.current_stream(device)
-    return torch.cuda.device(device), stream
+    if stream is not None:
+        if stream.device != device:
+            raise ValueError(f"stream on {stream.device}, tensors on {device}")
+        return _torch.cuda.stream(stream), stream
+    here = device.index == _torch.cuda.current_device()
+    # (the handle alone: a Stream object takes 1.8 us to make, more than the checks)
+    return (_HERE_CONTEXT if here else _torch.cuda.device(device),
+            _torch._C._cuda_getCurrentRawStream(device.index))
+
+
+_FLOAT_CODES = {} if _torch is None else {_torch.float32: HS_F32, _torch.bfloat16: HS_BF16}
 
 
 def _float_code(dtype, what: str) -> int:
-    import torch
-    if dtype == torch.float32:
-        return HS_F32
-    if dtype == torch.bfloat16:
-        return HS_BF16
-    raise TypeError(f"{what} must be float32 or bfloat16, not {dtype}")
+    code = _FLOAT_CODES.get(dtype)
+    if code is None:
+        raise TypeError(f"{what} must be float32 or bfloat16, not {dtype}")
+    return code
 
 
 def _tensor(t, what: str, device, shape=None, dtypes=None):
-    """Checks one contiguous device tensor."""
+    """Checks one contiguous device tensor (shape, dtypes: tuples)."""
     if t.device != device:
         raise ValueError(f"{what} is on {t.device}, not on {device}")
     if dtypes is not None and t.dtype not in dtypes:
         raise TypeError(f"{what} must be {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{what} has shape {tuple(t.shape)}, not {tuple(shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous")
     return t
+
+
+def _arg(t, what: str, device, shape, dtype):
+    """Address of one checked contiguous device tensor."""
+    if t.dtype is dtype and t.device == device and (shape is None or t.shape == shape) and \
+            t.is_contiguous():
+        return t.data_ptr()
+    return _tensor(t, what, device, shape, (dtype,)).data_ptr()
 
 
 def _rows_of(t, what: str):
@@ -848,7 +874,7 @@ class RowTable:
 def pack_rows(rows, group: int = 32, scale_dtype=None, stream=None) -> RowTable:
     """The packed 4-bit table of rows [n x dim] (float32 or bfloat16), dim a multiple of
     group (32, 64 or 128); scale_dtype bfloat16 (the default) or float32."""
-    import torch
+    torch = _torch
     scale_dtype = torch.bfloat16 if scale_dtype is None else scale_dtype
     if rows.dim() != 2:
         raise ValueError("rows must be 2-D")
@@ -858,7 +884,7 @@ def pack_rows(rows, group: int = 32, scale_dtype=None, stream=None) -> RowTable:
         raise ValueError(f"group {group} does not fit {rows.shape[1]} columns")
     n, d = rows.shape
     ctx, stream = _on(stream, rows.device)
-    with ctx, torch.cuda.stream(stream):
+    with ctx:
         data = torch.empty((n, d // 2), dtype=torch.uint8, device=rows.device)
         scales = torch.empty((n, d // group), dtype=scale_dtype, device=rows.device)
         hs_pack_rows(rows, code, n, d, group, sdt, data, scales, stream=stream)
@@ -866,9 +892,8 @@ def pack_rows(rows, group: int = 32, scale_dtype=None, stream=None) -> RowTable:
 
 
 def _ids(ids, device):
-    import torch
-    _tensor(ids, "ids", device, dtypes=(torch.int32, torch.int64))
-    return int(ids.dtype == torch.int64), ids.numel()
+    _tensor(ids, "ids", device, dtypes=(_torch.int32, _torch.int64))
+    return int(ids.dtype == _torch.int64), ids.numel()
 
 
 def embed(table: RowTable, ids, scale: float = 1.0, pad_id: int = -1, out_dtype=None, out=None,
@@ -877,17 +902,16 @@ def embed(table: RowTable, ids, scale: float = 1.0, pad_id: int = -1, out_dtype=
     int64), as ids.shape + [dim] in out_dtype (default: the table's type, bfloat16 for
     quantised tables).  Ids outside the table and pad_id give rows of zeros.  `out`:
     a contiguous tensor for the result."""
-    import torch
+    torch = _torch
     device = table.device
     is64, n = _ids(ids, device)
-    shape = tuple(ids.shape) + (table.dim,)
+    shape = ids.shape + (table.dim,)
     ctx, stream = _on(stream, device)
     with ctx:
         if out is None:
             if out_dtype is None:
                 out_dtype = torch.float32 if table.c.dtype == HS_F32 else torch.bfloat16
-            with torch.cuda.stream(stream):
-                out = torch.empty(shape, dtype=out_dtype, device=device)
+            out = torch.empty(shape, dtype=out_dtype, device=device)
         else:
             _tensor(out, "out", device, shape, None if out_dtype is None else (out_dtype,))
         hs_embed(table.c, ids, is64, n, scale, pad_id, out, _float_code(out.dtype, "out"),
@@ -901,25 +925,22 @@ def embed_grad(d_out, ids, rows: int, scale: float = 1.0, pad_id: int = -1, out_
     [dim] (float32 or bfloat16), the result [rows x dim] in out_dtype (default: that of
     d_out).  accumulate adds to `out`.  `ws`: a uint8 workspace of hs_embed_grad_bytes'
     size to use instead of a new one."""
-    import torch
+    torch = _torch
     device = d_out.device
     is64, n = _ids(ids, device)
     if d_out.dim() < 1:
         raise ValueError("d_out needs a column dimension")
     dim = d_out.shape[-1]
-    _tensor(d_out, "d_out", device, tuple(ids.shape) + (dim,))
+    _tensor(d_out, "d_out", device, ids.shape + (dim,))
     code = _float_code(d_out.dtype, "d_out")
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
     ctx, stream = _on(stream, device)
     with ctx:
-        if out is None or ws is None:
-            with torch.cuda.stream(stream):
-                if out is None:
-                    out = torch.empty((rows, dim), dtype=out_dtype or d_out.dtype, device=device)
-                if ws is None:
-                    ws = torch.empty(hs_embed_grad_bytes(n, rows, dim), dtype=torch.uint8,
-                                     device=device)
+        if out is None:
+            out = torch.empty((rows, dim), dtype=out_dtype or d_out.dtype, device=device)
+        if ws is None:
+            ws = torch.empty(hs_embed_grad_bytes(n, rows, dim), dtype=torch.uint8, device=device)
         _tensor(out, "out", device, (rows, dim), None if out_dtype is None else (out_dtype,))
         _tensor(ws, "ws", device)
         hs_embed_grad(d_out, code, ids, is64, n, rows, dim, scale, pad_id, int(accumulate), out,
@@ -931,7 +952,7 @@ def score_packed(table: RowTable, x, out_dtype=None, out=None, stream=None):
     """Products of rows x [m x dim] (float32 or bfloat16) with every row of a packed
     table, [m x table.rows] in out_dtype (default float32).  `out` may have a row
     stride above table.rows."""
-    import torch
+    torch = _torch
     device = table.device
     if table.c.dtype != HS_FP4_E2M1:
         raise TypeError("the table must be packed (pack_rows)")
@@ -943,11 +964,9 @@ def score_packed(table: RowTable, x, out_dtype=None, out=None, stream=None):
     ctx, stream = _on(stream, device)
     with ctx:
         if out is None:
-            with torch.cuda.stream(stream):
-                out = torch.empty((m, table.rows), dtype=out_dtype or torch.float32,
-                                  device=device)
+            out = torch.empty((m, table.rows), dtype=out_dtype or torch.float32, device=device)
         stride = _rows_of(out, "out")
-        if out.device != device or tuple(out.shape) != (m, table.rows) or \
+        if out.device != device or out.shape != (m, table.rows) or \
                 out_dtype not in (None, out.dtype):
             raise ValueError("out does not fit the table, x and out_dtype")
         hs_score_packed(table.c, x, code, m, out, _float_code(out.dtype, "out"), stride,
@@ -964,7 +983,7 @@ def adjust_scores(scores, allow=None, seen=None, seen_off=None, prompt_len=None,
     [rows] float32; bias_id [any] int32 and bias float32 with bias_off [rows + 1] int64;
     allow: int32 words, bit c % 32 of word c / 32 for column c, [words] for all rows or
     [rows x words].  `out` may be scores; by default a new tensor."""
-    import torch
+    torch = _torch
     device = scores.device
     stride = _rows_of(scores, "scores")
     code = _float_code(scores.dtype, "scores")
@@ -973,38 +992,37 @@ def adjust_scores(scores, allow=None, seen=None, seen_off=None, prompt_len=None,
         raise ValueError("seen and seen_off belong together")
     if not (bias_id is None) == (bias is None) == (bias_off is None):
         raise ValueError("bias_id, bias and bias_off belong together")
-    f32, i32, i64 = (torch.float32,), (torch.int32,), (torch.int64,)
+    f32, i32, i64 = torch.float32, torch.int32, torch.int64
+    per_row, offsets = (rows,), (rows + 1,)
     a = hs_adjust()
     if seen is not None:
-        a.seen = _ptr(_tensor(seen, "seen", device, dtypes=i32))
-        a.seen_off = _ptr(_tensor(seen_off, "seen_off", device, (rows + 1,), i64))
+        a.seen = _arg(seen, "seen", device, None, i32)
+        a.seen_off = _arg(seen_off, "seen_off", device, offsets, i64)
         a.n_seen = seen.numel()
     if bias_id is not None:
-        a.bias_id = _ptr(_tensor(bias_id, "bias_id", device, dtypes=i32))
-        a.bias = _ptr(_tensor(bias, "bias", device, bias_id.shape, f32))
-        a.bias_off = _ptr(_tensor(bias_off, "bias_off", device, (rows + 1,), i64))
+        a.bias_id = _arg(bias_id, "bias_id", device, None, i32)
+        a.bias = _arg(bias, "bias", device, bias_id.shape, f32)
+        a.bias_off = _arg(bias_off, "bias_off", device, offsets, i64)
         a.n_bias = bias_id.numel()
     if prompt_len is not None:
-        a.prompt_len = _ptr(_tensor(prompt_len, "prompt_len", device, (rows,), i32))
+        a.prompt_len = _arg(prompt_len, "prompt_len", device, per_row, i32)
     if repetition is not None:
-        a.repetition = _ptr(_tensor(repetition, "repetition", device, (rows,), f32))
+        a.repetition = _arg(repetition, "repetition", device, per_row, f32)
     if frequency is not None:
-        a.frequency = _ptr(_tensor(frequency, "frequency", device, (rows,), f32))
+        a.frequency = _arg(frequency, "frequency", device, per_row, f32)
     if presence is not None:
-        a.presence = _ptr(_tensor(presence, "presence", device, (rows,), f32))
+        a.presence = _arg(presence, "presence", device, per_row, f32)
     if allow is not None:
         words = (cols + 31) // 32
         if allow.dim() == 1:
-            _tensor(allow, "allow", device, (words,), i32)
+            a.allow = _arg(allow, "allow", device, (words,), i32)
         else:
-            _tensor(allow, "allow", device, (rows, words), i32)
+            a.allow = _arg(allow, "allow", device, (rows, words), i32)
             a.allow_stride = words
-        a.allow = _ptr(allow)
     ctx, stream = _on(stream, device)
     with ctx:
         if out is None:
-            with torch.cuda.stream(stream):
-                out = torch.empty((rows, cols), dtype=scores.dtype, device=device)
+            out = torch.empty((rows, cols), dtype=scores.dtype, device=device)
         elif out.device != device or out.shape != scores.shape or out.dtype != scores.dtype:
             raise ValueError("out does not fit scores")
         hs_adjust_scores(a, scores, stride, out, _rows_of(out, "out"), code, rows, cols,
@@ -1018,7 +1036,7 @@ def topk_rows(scores, k: int, out=None, ws=None, stream=None):
     ascending column; entries of -inf and NaN are never taken, slots left are (-inf, -1).
     `out`: the two tensors for the result, `ws`: a uint8 workspace of
     hs_topk_rows_bytes' size."""
-    import torch
+    torch = _torch
     device = scores.device
     stride = _rows_of(scores, "scores")
     code = _float_code(scores.dtype, "scores")
@@ -1026,13 +1044,11 @@ def topk_rows(scores, k: int, out=None, ws=None, stream=None):
     need = hs_topk_rows_bytes(rows, cols, k) if ws is None else 0
     ctx, stream = _on(stream, device)
     with ctx:
-        if out is None or ws is None:
-            with torch.cuda.stream(stream):
-                if out is None:
-                    out = (torch.empty((rows, k), dtype=torch.float32, device=device),
-                           torch.empty((rows, k), dtype=torch.int32, device=device))
-                if ws is None:
-                    ws = torch.empty(need, dtype=torch.uint8, device=device)
+        if out is None:
+            out = (torch.empty((rows, k), dtype=torch.float32, device=device),
+                   torch.empty((rows, k), dtype=torch.int32, device=device))
+        if ws is None:
+            ws = torch.empty(need, dtype=torch.uint8, device=device)
         _tensor(out[0], "out[0]", device, (rows, k), (torch.float32,))
         _tensor(out[1], "out[1]", device, (rows, k), (torch.int32,))
         _tensor(ws, "ws", device)
