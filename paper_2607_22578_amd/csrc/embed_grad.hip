@@ -5,12 +5,11 @@
 //           in ascending order; positions that stand for no token take the key
 //           `rows`, behind all others.  Up to kSmallMax positions in one workgroup;
 //           above, two launches per digit (counts per tile, scatter).
-//   starts  start[v] = first sorted place of token v (binary search per row).
 //   sums    the sorted places in chunks of at most 64: a wave adds up the rows of
 //           its chunk for one slice of columns, place after place, in registers, and
 //           writes a row whenever the token changes.  The work per wave does not depend
 //           on how often tokens occur.  Tokens that reach over a chunk's end leave
-//           partial sums.  The same launch writes the rows of tokens that do not occur.
+//           partial sums.
 //   join    partial sums of the tokens over several chunks, in chunk order.
 // Every row's additions are thus in an order that the sizes and ids fix.
 // Floor: dO once, dT once; the keys are small beside them.
@@ -35,10 +34,11 @@ constexpr int kSpanMany = 24;        // chunks that a workgroup instead of a wav
 struct GradWs {
   uint32_t *tok[2], *pos[2];   // [n] each: sorted keys and positions
   uint32_t *hist;              // [kTilesMax][kDigits]
-  uint32_t *start;             // [rows + 1]
   uint32_t *count;             // [2]: entries of the lists
   uint32_t *list[2];           // [chunks] each: chunks where a token over several chunks
                                // begins, with few (0) or many (1) of them
+  uint8_t *present;            // [rows, in fours]: 1 for tokens that occur (above kSmallMax
+                               // positions)
   float *part;                 // [2 x chunks][dim]: sums of the tokens over a chunk's
                                // start (0) and end (1)
 };
@@ -66,17 +66,69 @@ size_t layout(int64_t n, int64_t rows, int64_t dim, void *base, GradWs *w) {
   }
   if (w) w->hist = (uint32_t *)(p + at);
   at += (int64_t)kTilesMax * kDigits * 4;
-  if (w) w->start = (uint32_t *)(p + at);
-  at += up256((rows + 1) * 4);
   if (w) w->count = (uint32_t *)(p + at);
   at += 256;
   for (int i = 0; i < 2; ++i) {
     if (w) w->list[i] = (uint32_t *)(p + at);
     at += up256(chunks * 4);
   }
+  if (w) w->present = p + at;
+  if (n > kSmallMax) at += up256(rows);
   if (w) w->part = (float *)(p + at);
   at += up256(chunks * 2 * dim * 4);
   return (size_t)at;
+}
+
+// ---------------------------------------------------------------- rows of zeros
+//
+// The sort's launches leave most CUs idle, so further workgroups of theirs write the rows
+// of tokens that do not occur.
+struct Zeros {
+  uint8_t *table;
+  int64_t first, last;    // rows that are looked at, from a multiple of 4 on
+  int dim, elem, wide;    // wide: rows start and end on 16 bytes
+};
+
+// Zeros for the absent ones among rows r0 .. r0 + 3: a set bit each in `absent`.
+__device__ __forceinline__ void zero_four(const Zeros &z, int64_t r0, uint32_t absent) {
+  const int lane = threadIdx.x & 63;
+  if (z.wide) {
+    const int vecs = z.dim * z.elem / 16;
+    const u32x4v_t zero = {0u, 0u, 0u, 0u};
+    u32x4v_t *base = (u32x4v_t *)z.table + r0 * vecs;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if ((absent >> r) & 1u)
+        for (int i = lane; i < vecs; i += 64)
+          __builtin_nontemporal_store(zero, base + (int64_t)r * vecs + i);
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      if (!((absent >> r) & 1u)) continue;
+      const int64_t at = (r0 + r) * z.dim;
+      for (int i = lane; i < z.dim; i += 64) {
+        if (z.elem == 4)
+          ((uint32_t *)z.table)[at + i] = 0u;
+        else
+          ((uint16_t *)z.table)[at + i] = 0u;
+      }
+    }
+  }
+}
+
+// The share of workgroup `wg` of `wgs`, a wave for four rows.
+__device__ __forceinline__ void zero_rows(const Zeros &z, const uint8_t *present, int64_t wg,
+                                          int64_t wgs) {
+  const int waves = blockDim.x / 64;
+  for (int64_t r = z.first + (wg * waves + (threadIdx.x >> 6)) * 4; r < z.last;
+       r += wgs * waves * 4) {
+    const uint32_t here = *(const uint32_t *)(present + r);
+    uint32_t absent = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      absent |= r + i < z.last && !((here >> (8 * i)) & 255u) ? 1u << i : 0u;
+    zero_four(z, r, __builtin_amdgcn_readfirstlane(absent));
+  }
 }
 
 // ---------------------------------------------------------------- sort
@@ -124,13 +176,38 @@ __device__ __forceinline__ uint32_t scan_digits(uint32_t v, uint32_t *sums) {
 
 // All passes in one workgroup, keys and positions in LDS; 16 waves, each with a
 // contiguous share and its own digit counters (made exclusive over digits and waves).
+// The workgroups behind the first write the rows of zeros, slabs of `slab` rows each: they
+// find the tokens of a slab themselves.
 __global__ __launch_bounds__(kSmallWaves * 64) void grad_sort_small(
     const void *__restrict__ ids, int is64, int n, int64_t rows, int64_t pad, int bits, int passes,
-    uint32_t *__restrict__ tok, uint32_t *__restrict__ pos) {
+    uint32_t *__restrict__ tok, uint32_t *__restrict__ pos, uint32_t *__restrict__ count, Zeros z,
+    int slab) {
   __shared__ uint32_t key[2][kSmallMax], val[2][kSmallMax];
   __shared__ uint32_t cnt[kSmallWaves][kDigits];
   __shared__ uint32_t sums[kDigits / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (blockIdx.x == 0 && tid < 2) count[tid] = 0u;
+  if (blockIdx.x > 0) {
+    uint32_t *occur = key[0];   // a bit per row of the slab (at most 32 kSmallMax)
+    for (int64_t first = (int64_t)(blockIdx.x - 1) * slab; first < z.last;
+         first += (int64_t)(gridDim.x - 1) * slab) {
+      const int64_t last = first + slab < z.last ? first + slab : z.last;
+      for (int i = tid; i < slab / 32; i += kSmallWaves * 64) occur[i] = 0u;
+      __syncthreads();
+      for (int i = tid; i < n; i += kSmallWaves * 64) {
+        const int64_t v = token_key(ids, is64, i, rows, pad);
+        if (v >= first && v < last) atomicOr(&occur[(v - first) >> 5], 1u << (v & 31));
+      }
+      __syncthreads();
+      for (int64_t r = first + wave * 4; r < last; r += kSmallWaves * 4) {
+        uint32_t absent = ~(occur[(r - first) >> 5] >> (r & 31)) & 15u;
+        if (last - r < 4) absent &= (1u << (last - r)) - 1u;
+        zero_four(z, r, __builtin_amdgcn_readfirstlane(absent));
+      }
+      __syncthreads();
+    }
+    return;
+  }
   for (int i = tid; i < n; i += kSmallWaves * 64) {
     key[0][i] = token_key(ids, is64, i, rows, pad);
     val[0][i] = (uint32_t)i;
@@ -186,12 +263,26 @@ __global__ __launch_bounds__(kSmallWaves * 64) void grad_sort_small(
   }
 }
 
-// Digit counts of one tile; the first pass makes the keys from the ids.
+// Digit counts of one tile; the first pass makes the keys from the ids, and clears the
+// marks of tokens that occur and the lists.  Workgroups from `tiles` on write rows of zeros (not in
+// the first pass).
 template <bool FIRST>
 __global__ __launch_bounds__(kSortWaves * 64) void grad_count(
     const void *__restrict__ ids, int is64, const uint32_t *__restrict__ tok, int64_t n,
-    int64_t tile, int64_t rows, int64_t pad, int bits, int shift, uint32_t *__restrict__ hist) {
+    int64_t tile, int tiles, int64_t rows, int64_t pad, int bits, int shift,
+    uint32_t *__restrict__ hist, uint8_t *__restrict__ present, uint32_t *__restrict__ count,
+    Zeros z) {
   __shared__ uint32_t cnt[kDigits];
+  if ((int)blockIdx.x >= tiles) {
+    zero_rows(z, present, (int64_t)blockIdx.x - tiles, (int64_t)gridDim.x - tiles);
+    return;
+  }
+  if (FIRST) {
+    if (blockIdx.x == 0 && threadIdx.x < 2) count[threadIdx.x] = 0u;
+    for (int64_t i = (int64_t)blockIdx.x * kSortWaves * 64 + threadIdx.x; i < (rows + 3) / 4;
+         i += (int64_t)tiles * kSortWaves * 64)
+      ((uint32_t *)present)[i] = 0u;
+  }
   if (threadIdx.x < kDigits) cnt[threadIdx.x] = 0u;
   __syncthreads();
   const int64_t lo = (int64_t)blockIdx.x * tile, hi = lo + tile < n ? lo + tile : n;
@@ -208,16 +299,22 @@ __global__ __launch_bounds__(kSortWaves * 64) void grad_count(
 // Stable scatter of one tile.  The tile's first place of each digit comes straight
 // from the counts of all tiles: two threads per digit, 32 reads each at most, all in
 // flight at once (with 128 tiles and 8 in flight they were most of the launch: 16 us for
-// 262,144 positions).
+// 262,144 positions).  The first pass also marks the tokens that occur; workgroups from
+// `tiles` on write rows of zeros (not in the first pass).
 template <bool FIRST>
 __global__ __launch_bounds__(kSortWaves * 64) void grad_scatter(
     const void *__restrict__ ids, int is64, const uint32_t *__restrict__ tok,
     const uint32_t *__restrict__ pos, int64_t n, int64_t tile, int tiles, int64_t rows,
     int64_t pad, int bits, int shift, const uint32_t *__restrict__ hist,
-    uint32_t *__restrict__ tok_out, uint32_t *__restrict__ pos_out) {
+    uint32_t *__restrict__ tok_out, uint32_t *__restrict__ pos_out,
+    uint8_t *__restrict__ present, Zeros z) {
   __shared__ uint32_t cnt[kSortWaves][kDigits];
   __shared__ uint32_t other[2][kDigits];
   __shared__ uint32_t sums[kDigits / 64];
+  if ((int)blockIdx.x >= tiles) {
+    zero_rows(z, present, (int64_t)blockIdx.x - tiles, (int64_t)gridDim.x - tiles);
+    return;
+  }
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const uint32_t mask = (1u << bits) - 1u;
   const int64_t lo = (int64_t)blockIdx.x * tile, hi = lo + tile < n ? lo + tile : n;
@@ -237,6 +334,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void grad_scatter(
       if (i < whi) {
         key[u] = FIRST ? token_key(ids, is64, i, rows, pad) : tok[i];
         val[u] = FIRST ? (uint32_t)i : pos[i];
+        if (FIRST && key[u] < (uint32_t)rows) present[key[u]] = 1;
       }
     }
   };
@@ -292,26 +390,6 @@ __global__ __launch_bounds__(kSortWaves * 64) void grad_scatter(
       if (in && (same >> lane) == 1ull) cnt[wave][d] += (uint32_t)__popcll(same);
       wave_fence();
     }
-  }
-}
-
-// start[v] for v <= rows: the first sorted place whose token is v or above.  Also
-// empties the lists.
-__global__ __launch_bounds__(256) void grad_starts(const uint32_t *__restrict__ tok, int64_t n,
-                                                   int64_t rows, uint32_t *__restrict__ start,
-                                                   uint32_t *__restrict__ count) {
-  if (blockIdx.x == 0 && threadIdx.x < 2) count[threadIdx.x] = 0u;
-  for (int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x; v <= rows;
-       v += (int64_t)gridDim.x * 256) {
-    int64_t a = 0, b = n;
-    while (a < b) {
-      const int64_t m = (a + b) >> 1;
-      if (tok[m] < (uint32_t)v)
-        a = m + 1;
-      else
-        b = m;
-    }
-    start[v] = (uint32_t)a;
   }
 }
 
@@ -401,22 +479,15 @@ struct Slice {
 template <int DT, int OT, bool WIDE>
 __global__ __launch_bounds__(256) void grad_sums(
     const uint8_t *__restrict__ grad, const uint32_t *__restrict__ tok,
-    const uint32_t *__restrict__ pos, const uint32_t *__restrict__ start, int64_t n, int64_t rows,
-    int dim, int places, int64_t chunks, int slices, int64_t sum_blocks, float scale, int add,
+    const uint32_t *__restrict__ pos, int64_t n, int64_t rows, int dim, int places,
+    int64_t chunks, int slices, int64_t sum_blocks, float scale, int add,
     float *__restrict__ part, uint32_t *__restrict__ count, uint32_t *__restrict__ few,
-    uint32_t *__restrict__ many, uint8_t *__restrict__ table) {
+    uint32_t *__restrict__ many, uint8_t *__restrict__ table,
+    const uint8_t *__restrict__ present, Zeros z) {
   using S = Slice<DT, WIDE>;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if ((int64_t)blockIdx.x >= sum_blocks) {
-    // rows of tokens that do not occur: a wave per row and slice
-    float zero[S::V] = {};
-    const int64_t all = rows * slices;
-    for (int64_t t = ((int64_t)blockIdx.x - sum_blocks) * 4 + wave; t < all;
-         t += ((int64_t)gridDim.x - sum_blocks) * 4) {
-      const int64_t r = t / slices;
-      if (start[r] == start[r + 1])
-        S::template write<OT>(table, r, (int)(t - r * slices) * S::kCols, lane, dim, 0, zero);
-    }
+    zero_rows(z, present, (int64_t)blockIdx.x - sum_blocks, (int64_t)gridDim.x - sum_blocks);
     return;
   }
   const int64_t task = (int64_t)blockIdx.x * 4 + wave;
@@ -473,8 +544,8 @@ __global__ __launch_bounds__(256) void grad_sums(
   } else if (cur == next) {
     S::part(part + (c * 2 + 1) * dim, col0, lane, dim, acc);
     if (col0 == 0 && lane == 0) {
-      const int64_t span = ((int64_t)start[cur + 1] - 1) / places - c;
-      const int l = span >= kSpanMany ? 1 : 0;
+      const int64_t far = (c + kSpanMany) * places;
+      const int l = far < n && tok[far] == cur ? 1 : 0;
       (l ? many : few)[atomicAdd(&count[l], 1u)] = (uint32_t)c;
     }
   } else {
@@ -485,104 +556,92 @@ __global__ __launch_bounds__(256) void grad_sums(
 }
 
 // Tokens over several chunks: the sum at the end of the chunk where the token begins
-// and those at the start of the following ones, 256 columns at a time.  A wave joins
-// a few chunks, in order; a workgroup many, in four contiguous shares whose sums are
-// added in order.
+// and those at the start of the following ones.  A wave joins a few chunks, 256 columns at
+// a time, in order; a workgroup many, 64 columns at a time, in four contiguous shares
+// whose sums are added in order.
 template <int OT>
-__device__ __forceinline__ void join_write(uint8_t *table, int64_t t, int col, int dim,
-                                           float scale, int add, const float *v) {
+__device__ __forceinline__ void join_write(uint8_t *table, int64_t t, int c, int dim, float x,
+                                           int add) {
   uint8_t *row = table + t * dim * (OT == HS_F32 ? 4 : 2);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int c = col + j * 64;
-    if (c < dim) {
-      const float x = v[j] * scale;
-      store_col<OT>(row, c, add ? x + load_col<OT>(row, c) : x);
-    }
-  }
-}
-
-__device__ __forceinline__ void join_sum(const float *part, int64_t a, int64_t b, int col, int dim,
-                                         float *v) {
-#pragma unroll 4
-  for (int64_t k = a; k < b; ++k) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int c = col + j * 64;
-      v[j] += part[k * 2 * dim + (c < dim ? c : 0)];
-    }
-  }
+  if (c < dim) store_col<OT>(row, c, add ? x + load_col<OT>(row, c) : x);
 }
 
 template <int OT>
 __global__ __launch_bounds__(256) void grad_join(
-    const uint32_t *__restrict__ tok, const uint32_t *__restrict__ start, int dim, int places,
-    int col_blocks, float scale, int add, const uint32_t *__restrict__ count,
-    const uint32_t *__restrict__ few, const uint32_t *__restrict__ many,
-    const float *__restrict__ part, uint8_t *__restrict__ table) {
-  __shared__ float sums[4][256];
+    const uint32_t *__restrict__ tok, int64_t n, int dim, int places, int64_t chunks,
+    float scale, int add, const uint32_t *__restrict__ count, const uint32_t *__restrict__ few,
+    const uint32_t *__restrict__ many, const float *__restrict__ part,
+    uint8_t *__restrict__ table) {
+  __shared__ float sums[4][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t n_many = (int64_t)count[1] * col_blocks, n_few = (int64_t)count[0] * col_blocks;
+  const int many_blocks = (dim + 63) / 64, few_blocks = (dim + 255) / 256;
+  const int64_t n_many = (int64_t)count[1] * many_blocks, n_few = (int64_t)count[0] * few_blocks;
   for (int64_t task = blockIdx.x; task < n_many; task += gridDim.x) {
-    const int64_t e = task / col_blocks, c = many[e];
-    const int col = (int)(task - e * col_blocks) * 256 + lane;
+    const int64_t e = task / many_blocks, c = many[e];
+    const int col = (int)(task - e * many_blocks) * 64 + lane, cc = col < dim ? col : 0;
     const uint32_t t = tok[(c + 1) * places - 1];
-    const int64_t c1 = ((int64_t)start[t + 1] - 1) / places;   // its last chunk
-    const int64_t share = (c1 - c + 3) / 4;
-    const int64_t a = c + 1 + wave * share, b = a + share < c1 + 1 ? a + share : c1 + 1;
-    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (wave == 0) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = col + j * 64 < dim ? part[(c * 2 + 1) * dim + col + j * 64] : 0.0f;
+    // its last chunk: between lo, whose first token it is, and hi, 64 tries at a time
+    int64_t lo = c + kSpanMany, hi = chunks;
+    while (hi - lo > 1) {
+      const int64_t step = (hi - lo + 63) / 64, k = lo + (lane + 1) * step;
+      lo += step * __popcll(__builtin_amdgcn_ballot_w64(k < hi && tok[k * places] == t));
+      hi = hi < lo + step ? hi : lo + step;
     }
-    join_sum(part, a, b, col, dim, v);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sums[wave][j * 64 + lane] = v[j];
+    const int64_t c1 = lo, share = (c1 - c + 3) / 4;
+    const int64_t a = c + 1 + wave * share, b = a + share < c1 + 1 ? a + share : c1 + 1;
+    float v = wave == 0 ? part[(c * 2 + 1) * dim + cc] : 0.0f;
+    // (16 in flight: with four, a token in 15,000 of 262,144 places took most of the launch)
+#pragma unroll 16
+    for (int64_t k = a; k < b; ++k) v += part[k * 2 * dim + cc];
+    sums[wave][lane] = v;
     __syncthreads();
     if (wave == 0) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = j * 64 + lane;
-        v[j] = ((sums[0][i] + sums[1][i]) + sums[2][i]) + sums[3][i];
-      }
-      join_write<OT>(table, t, col, dim, scale, add, v);
+      v = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
+      join_write<OT>(table, t, col, dim, v * scale, add);
     }
     __syncthreads();
   }
   for (int64_t task = (int64_t)blockIdx.x * 4 + wave; task < n_few; task += (int64_t)gridDim.x * 4) {
-    const int64_t e = task / col_blocks, c = few[e];
-    const int col = (int)(task - e * col_blocks) * 256 + lane;
+    const int64_t e = task / few_blocks, c = few[e];
+    const int col = (int)(task - e * few_blocks) * 256 + lane;
     const uint32_t t = tok[(c + 1) * places - 1];
-    const int64_t c1 = ((int64_t)start[t + 1] - 1) / places;
+    const int64_t k0 = c + 1 + lane;   // chunks that begin with it: below kSpanMany of them
+    const int64_t c1 = c + __popcll(__builtin_amdgcn_ballot_w64(
+                               lane < kSpanMany && k0 < chunks && tok[k0 * places] == t));
     float v[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = col + j * 64 < dim ? part[(c * 2 + 1) * dim + col + j * 64] : 0.0f;
-    join_sum(part, c + 1, c1 + 1, col, dim, v);
-    join_write<OT>(table, t, col, dim, scale, add, v);
+    for (int j = 0; j < 4; ++j)
+      v[j] = part[(c * 2 + 1) * dim + (col + j * 64 < dim ? col + j * 64 : 0)];
+#pragma unroll 4
+    for (int64_t k = c + 1; k <= c1; ++k) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] += part[k * 2 * dim + (col + j * 64 < dim ? col + j * 64 : 0)];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) join_write<OT>(table, t, col + j * 64, dim, v[j] * scale, add);
   }
 }
 
 template <int DT, int OT>
 hipError_t launch_sums(const GradWs &w, int side, const void *grad, int64_t n, int64_t rows,
-                       int64_t dim, float scale, int add, void *table, hipStream_t st) {
+                       int64_t dim, float scale, int add, void *table, const Zeros &z, int zero_wgs,
+                       hipStream_t st) {
   constexpr int V = DT == HS_F32 ? 4 : 8;
   const int places = chunk_places(n, dim);
   const int64_t chunks = (n + places - 1) / places;
   const int slices = (int)((dim + 64 * V - 1) / (64 * V));
   const bool wide = dim % V == 0 && ((uintptr_t)grad % 16) == 0 && ((uintptr_t)table % 16) == 0;
   const int64_t sum_blocks = (chunks * slices + 3) / 4;
-  int64_t zero_blocks = add ? 0 : (rows * slices + 3) / 4;
-  if (zero_blocks > 4096) zero_blocks = 4096;
   hipLaunchKernelGGL((wide ? grad_sums<DT, OT, true> : grad_sums<DT, OT, false>),
-                     dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, st,
-                     (const uint8_t *)grad, w.tok[side], w.pos[side], w.start, n, rows, (int)dim,
-                     places, chunks, slices, sum_blocks, scale, add, w.part, w.count, w.list[0],
-                     w.list[1], (uint8_t *)table);
+                     dim3((unsigned)(sum_blocks + zero_wgs)), dim3(256), 0, st,
+                     (const uint8_t *)grad, w.tok[side], w.pos[side], n, rows, (int)dim, places,
+                     chunks, slices, sum_blocks, scale, add, w.part, w.count, w.list[0],
+                     w.list[1], (uint8_t *)table, w.present, z);
   if (chunks > 1) {
-    const int col_blocks = (int)((dim + 255) / 256);
-    const int64_t tasks = ((chunks - 1) * col_blocks + 3) / 4;   // (as many at most, in waves)
+    // (as many tasks at most, in waves)
+    const int64_t tasks = ((chunks - 1) * ((dim + 255) / 256) + 3) / 4;
     hipLaunchKernelGGL(grad_join<OT>, dim3((unsigned)(tasks < 1024 ? tasks : 1024)), dim3(256), 0,
-                       st, w.tok[side], w.start, (int)dim, places, col_blocks, scale, add, w.count,
+                       st, w.tok[side], n, (int)dim, places, chunks, scale, add, w.count,
                        w.list[0], w.list[1], w.part, (uint8_t *)table);
   }
   return hipGetLastError();
@@ -605,44 +664,75 @@ hipError_t launch_embed_grad(const void *grad, int grad_dtype, const void *ids, 
   const int passes = (key_bits + kDigitBits - 1) / kDigitBits;
   const int bits = (key_bits + passes - 1) / passes;
   int side = 0;
-  if (n > 0 && n <= kSmallMax) {
-    hipLaunchKernelGGL(grad_sort_small, dim3(1), dim3(kSmallWaves * 64), 0, st, ids, is64, (int)n,
-                       rows, pad, bits, passes, w.tok[0], w.pos[0]);
-  } else if (n > 0) {
+  const int elem = table_dtype == HS_F32 ? 4 : 2;
+  const int64_t stop = add ? 0 : rows;   // rows of zeros are written below it
+  const int wide = (dim * elem) % 16 == 0 && ((uintptr_t)table % 16) == 0;
+  const Zeros all = {(uint8_t *)table, 0, stop, (int)dim, elem, wide};
+  Zeros part[3] = {all, all, all};       // of the second count and scatter, of the sums
+  int zero_wgs[3] = {0, 0, 0};
+  if (n <= kSmallMax) {
+    // slabs: one workgroup for each CU but the sort's; at most as many rows as the bitmap
+    // holds
+    int64_t slab = ((stop + 254) / 255 + 31) / 32 * 32;
+    slab = slab < 32 ? 32 : slab > 32 * kSmallMax ? 32 * kSmallMax : slab;
+    const int64_t wgs = (stop + slab - 1) / slab;
+    hipLaunchKernelGGL(grad_sort_small, dim3(1 + (unsigned)(wgs < 255 ? wgs : 255)),
+                       dim3(kSmallWaves * 64), 0, st, ids, is64, (int)n, rows, pad, bits, passes,
+                       w.tok[0], w.pos[0], w.count, all, (int)slab);
+    part[2].last = 0;
+  } else {
     int64_t tiles = (n + kTileMin - 1) / kTileMin;
     if (tiles > kTilesMax) tiles = kTilesMax;
     int64_t tile = (n + tiles - 1) / tiles;
     tile = (tile + kSortWaves * 64 - 1) / (kSortWaves * 64) * (kSortWaves * 64);
     tiles = (n + tile - 1) / tile;
-    const dim3 g((unsigned)tiles), b(kSortWaves * 64);
+    // the rows of zeros: most behind the second pass, whose launches take 5 and 11 us
+    // without them (262,144 positions) and leave the memory idle
+    if (passes > 1) {
+      part[0].last = stop / 5 / 4 * 4;
+      part[1].first = part[0].last;
+      part[1].last = stop * 13 / 20 / 4 * 4;
+      part[2].first = part[1].last;
+    }
+    for (int i = passes > 1 ? 0 : 2; i < 3; ++i) {
+      const int64_t waves = (part[i].last - part[i].first + 3) / 4;
+      const int64_t wgs = (waves + (i < 2 ? kSortWaves : 4) - 1) / (i < 2 ? kSortWaves : 4);
+      zero_wgs[i] = (int)(wgs < 1024 ? wgs : 1024);
+    }
+    const dim3 b(kSortWaves * 64);
     for (int p = 0; p < passes; ++p) {
       const int shift = p * bits;
+      // (with more than two passes the later ones write no zeros)
+      const int zc = p == 1 ? zero_wgs[0] : 0, zs = p == 1 ? zero_wgs[1] : 0;
+      const dim3 gc((unsigned)(tiles + zc)), gs((unsigned)(tiles + zs));
       if (p == 0) {
-        hipLaunchKernelGGL(grad_count<true>, g, b, 0, st, ids, is64, nullptr, n, tile, rows, pad,
-                           bits, shift, w.hist);
-        hipLaunchKernelGGL(grad_scatter<true>, g, b, 0, st, ids, is64, nullptr, nullptr, n, tile,
-                           (int)tiles, rows, pad, bits, shift, w.hist, w.tok[0], w.pos[0]);
+        hipLaunchKernelGGL(grad_count<true>, gc, b, 0, st, ids, is64, nullptr, n, tile, (int)tiles,
+                           rows, pad, bits, shift, w.hist, w.present, w.count, part[0]);
+        hipLaunchKernelGGL(grad_scatter<true>, gs, b, 0, st, ids, is64, nullptr, nullptr, n, tile,
+                           (int)tiles, rows, pad, bits, shift, w.hist, w.tok[0], w.pos[0],
+                           w.present, part[1]);
       } else {
-        hipLaunchKernelGGL(grad_count<false>, g, b, 0, st, ids, is64, w.tok[side], n, tile, rows,
-                           pad, bits, shift, w.hist);
-        hipLaunchKernelGGL(grad_scatter<false>, g, b, 0, st, ids, is64, w.tok[side], w.pos[side],
+        hipLaunchKernelGGL(grad_count<false>, gc, b, 0, st, ids, is64, w.tok[side], n, tile,
+                           (int)tiles, rows, pad, bits, shift, w.hist, w.present, w.count, part[0]);
+        hipLaunchKernelGGL(grad_scatter<false>, gs, b, 0, st, ids, is64, w.tok[side], w.pos[side],
                            n, tile, (int)tiles, rows, pad, bits, shift, w.hist, w.tok[side ^ 1],
-                           w.pos[side ^ 1]);
+                           w.pos[side ^ 1], w.present, part[1]);
         side ^= 1;
       }
     }
   }
-  int64_t blocks = (rows + 256) / 256;
-  if (blocks > 4096) blocks = 4096;
-  hipLaunchKernelGGL(grad_starts, dim3((unsigned)blocks), dim3(256), 0, st, w.tok[side], n, rows,
-                     w.start, w.count);
+  if (n == 0) return hipGetLastError();
   if (grad_dtype == HS_F32)
     return table_dtype == HS_F32
-               ? launch_sums<HS_F32, HS_F32>(w, side, grad, n, rows, dim, scale, add, table, st)
-               : launch_sums<HS_F32, HS_BF16>(w, side, grad, n, rows, dim, scale, add, table, st);
+               ? launch_sums<HS_F32, HS_F32>(w, side, grad, n, rows, dim, scale, add, table,
+                                              part[2], zero_wgs[2], st)
+               : launch_sums<HS_F32, HS_BF16>(w, side, grad, n, rows, dim, scale, add, table,
+                                              part[2], zero_wgs[2], st);
   return table_dtype == HS_F32
-             ? launch_sums<HS_BF16, HS_F32>(w, side, grad, n, rows, dim, scale, add, table, st)
-             : launch_sums<HS_BF16, HS_BF16>(w, side, grad, n, rows, dim, scale, add, table, st);
+             ? launch_sums<HS_BF16, HS_F32>(w, side, grad, n, rows, dim, scale, add, table,
+                                              part[2], zero_wgs[2], st)
+             : launch_sums<HS_BF16, HS_BF16>(w, side, grad, n, rows, dim, scale, add, table,
+                                              part[2], zero_wgs[2], st);
 }
 
 }  // namespace hs
