@@ -78,7 +78,7 @@ struct __align__(16) Table {
 // threads that see room at the same time: the table never fills up, so searches end
 static_assert(kMarkedMax + kThreads < kSlots, "an empty slot is always left");
 
-// WIDE: rows start on 16 bytes and have at least that.
+// WIDE: rows have 16 bytes at least.
 template <int DT, bool WIDE>
 __global__ __launch_bounds__(kThreads) void adjust_kernel(
     hs_adjust a, const uint8_t *__restrict__ in, int64_t stride, uint8_t *__restrict__ out,
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(
     if (b0 + tid < b1) bias0 = a.bias_id[b0 + tid];
     RawCols<DT, C> raw[U];
     uint32_t bits[U];
-    const uint32_t *words = allow ? allow : (const uint32_t *)src;
+    const uint32_t *words = allow ? allow : (const uint32_t *)(((uintptr_t)src + 3) & ~(uintptr_t)3);
     for (int64_t lo = first, hi = last; lo < last; lo = hi, hi = last) {
       auto load = [&](int v0) {
 #pragma unroll
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(
             }
 #pragma unroll
             for (int j = 0; j < C; ++j) x[j] = (ok[u] >> j) & 1u ? x[j] : -__builtin_inff();
-            *(u32x4v_t *)(dst + (lo + c) * ES) = round_cols<DT, C>(x);
+            store_cols(dst + (lo + c) * ES, round_cols<DT, C>(x));
           }
         }
       }
@@ -246,9 +246,7 @@ hipError_t launch_adjust(const hs_adjust *a, const void *in, int64_t stride, voi
   range = (range + kRangeMin - 1) / kRangeMin * kRangeMin;
   range = range < kRangeMin ? kRangeMin : range > kRangeMax ? kRangeMax : range;
   const int64_t ranges = (n_cols + range - 1) / range, items = n_rows * ranges;
-  const bool wide = ((uintptr_t)in % 16) == 0 && ((uintptr_t)out % 16) == 0 &&
-                    n_cols * es >= 16 &&
-                    (n_rows == 1 || (stride * es % 16 == 0 && out_stride * es % 16 == 0));
+  const bool wide = n_cols * es >= 16;
   const dim3 g((unsigned)(items < (1 << 20) ? items : (1 << 20))), b(kThreads);
   auto kernel = dtype == HS_F32 ? (wide ? adjust_kernel<HS_F32, true> : adjust_kernel<HS_F32, false>)
                                 : (wide ? adjust_kernel<HS_BF16, true>

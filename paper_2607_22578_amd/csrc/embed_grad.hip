@@ -19,7 +19,7 @@ namespace hs {
 
 namespace {
 
-constexpr int kSmallMax = 4096;      // positions that one workgroup sorts
+constexpr int kSmallMax = 10240;     // positions that one workgroup sorts: 152 KiB of LDS
 constexpr int kSmallWaves = 16;
 constexpr int kSortWaves = 16;       // per tile
 constexpr int kRounds = 4;           // keys per lane held in registers
@@ -86,32 +86,24 @@ size_t layout(int64_t n, int64_t rows, int64_t dim, void *base, GradWs *w) {
 struct Zeros {
   uint8_t *table;
   int64_t first, last;    // rows that are looked at, from a multiple of 4 on
-  int dim, elem, wide;    // wide: rows start and end on 16 bytes
+  int dim, elem;
 };
 
 // Zeros for the absent ones among rows r0 .. r0 + 3: a set bit each in `absent`.
 __device__ __forceinline__ void zero_four(const Zeros &z, int64_t r0, uint32_t absent) {
   const int lane = threadIdx.x & 63;
-  if (z.wide) {
-    const int vecs = z.dim * z.elem / 16;
-    const u32x4v_t zero = {0u, 0u, 0u, 0u};
-    u32x4v_t *base = (u32x4v_t *)z.table + r0 * vecs;
+  const int vecs = z.dim * z.elem / 16, rest = z.dim * z.elem % 16 / z.elem;
+  const u32x4v_t zero = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if ((absent >> r) & 1u)
-        for (int i = lane; i < vecs; i += 64)
-          __builtin_nontemporal_store(zero, base + (int64_t)r * vecs + i);
-  } else {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      if (!((absent >> r) & 1u)) continue;
-      const int64_t at = (r0 + r) * z.dim;
-      for (int i = lane; i < z.dim; i += 64) {
-        if (z.elem == 4)
-          ((uint32_t *)z.table)[at + i] = 0u;
-        else
-          ((uint16_t *)z.table)[at + i] = 0u;
-      }
+  for (int r = 0; r < 4; ++r) {
+    if (!((absent >> r) & 1u)) continue;
+    uint8_t *row = z.table + (r0 + r) * z.dim * z.elem;
+    for (int i = lane; i < vecs; i += 64) stream_cols(row + i * 16, zero);
+    if (lane < rest) {
+      if (z.elem == 4)
+        ((uint32_t *)row)[vecs * 4 + lane] = 0u;
+      else
+        ((uint16_t *)row)[vecs * 8 + lane] = 0u;
     }
   }
 }
@@ -182,7 +174,8 @@ __global__ __launch_bounds__(kSmallWaves * 64) void grad_sort_small(
     const void *__restrict__ ids, int is64, int n, int64_t rows, int64_t pad, int bits, int passes,
     uint32_t *__restrict__ tok, uint32_t *__restrict__ pos, uint32_t *__restrict__ count, Zeros z,
     int slab) {
-  __shared__ uint32_t key[2][kSmallMax], val[2][kSmallMax];
+  __shared__ uint32_t key[2][kSmallMax];
+  __shared__ uint16_t val[2][kSmallMax];
   __shared__ uint32_t cnt[kSmallWaves][kDigits];
   __shared__ uint32_t sums[kDigits / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -210,7 +203,7 @@ __global__ __launch_bounds__(kSmallWaves * 64) void grad_sort_small(
   }
   for (int i = tid; i < n; i += kSmallWaves * 64) {
     key[0][i] = token_key(ids, is64, i, rows, pad);
-    val[0][i] = (uint32_t)i;
+    val[0][i] = (uint16_t)i;
   }
   const int share = ((n + kSmallWaves - 1) / kSmallWaves + 63) & ~63;
   const int lo = wave * share, hi = lo + share < n ? lo + share : n;
@@ -395,55 +388,47 @@ __global__ __launch_bounds__(kSortWaves * 64) void grad_scatter(
 
 // ---------------------------------------------------------------- sums
 //
-// V columns per lane and slice: consecutive ones where 16-byte accesses fit (WIDE),
-// else 64 apart.
-template <int DT, bool WIDE>
+// V consecutive columns per lane and slice.  A row's last lane takes the last V columns,
+// some of them its neighbour's too: both get the same sums, in the same instructions.
+// Rows of less than V columns are one lane's.
+template <int DT>
 struct Slice {
   static constexpr int V = DT == HS_F32 ? 4 : 8;
   static constexpr int kCols = 64 * V;
 
-  __device__ static __forceinline__ void load(const uint8_t *row, int col0, int lane, int dim,
-                                              float *v) {
-    if constexpr (WIDE) {
-      const int c = col0 + lane * V;
-      if (c < dim) {
-        RawCols<DT, V> raw;
-        raw.load(row, c);
-        raw.decode(v);
-      } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = 0.0f;
-      }
+  // The lane's first column; dim and above: none.
+  __device__ static __forceinline__ int column(int slice, int lane, int dim) {
+    const int c = slice * kCols + lane * V;
+    return c < dim && c + V > dim && dim >= V ? dim - V : c;
+  }
+
+  __device__ static __forceinline__ void load(const uint8_t *row, int c, int dim, float *v) {
+    if (dim >= V) {   // (the same for every lane; those without columns load the first)
+      RawCols<DT, V> raw;
+      raw.load(row, c < dim ? c : 0);
+      raw.decode(v);
     } else {
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int c = col0 + j * 64 + lane;
-        v[j] = c < dim ? load_col<DT>(row, c) : 0.0f;
-      }
+      for (int j = 0; j < V; ++j) v[j] = c + j < dim ? load_col<DT>(row, c + j) : 0.0f;
     }
   }
 
-  // partial sums keep the lane's columns in the same places
-  __device__ static __forceinline__ void part(float *row, int col0, int lane, int dim,
-                                              const float *v) {
+  __device__ static __forceinline__ void part(float *row, int c, int dim, const float *v) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = WIDE ? col0 + lane * V + j : col0 + j * 64 + lane;
-      if (c < dim) row[c] = v[j];
-    }
+    for (int j = 0; j < V; ++j)
+      if (c + j < dim) row[c + j] = v[j];
   }
 
+  // table[r] = (add: +=) scale * v
   template <int OT>
-  __device__ static __forceinline__ void write(uint8_t *table, int64_t r, int col0, int lane,
-                                               int dim, int add, const float *v) {
+  __device__ static __forceinline__ void write(uint8_t *table, int64_t r, int c, int dim,
+                                               float scale, int add, const float *v) {
     constexpr int OB = OT == HS_F32 ? 4 : 2;
     uint8_t *row = table + r * (int64_t)dim * OB;
-    if constexpr (WIDE) {
-      const int c = col0 + lane * V;
-      if (c >= dim) return;
+    if (c + V <= dim) {
       float o[V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) o[j] = v[j];
+      for (int j = 0; j < V; ++j) o[j] = v[j] * scale;
       if (add) {
         RawCols<OT, V> raw;
         float old[V];
@@ -455,28 +440,25 @@ struct Slice {
       if constexpr (OT == HS_F32) {
 #pragma unroll
         for (int j = 0; j < V; j += 4)
-          __builtin_nontemporal_store(round_cols<HS_F32, 4>(o + j),
-                                      (u32x4v_t *)(row + (int64_t)(c + j) * 4));
+          stream_cols(row + (int64_t)(c + j) * 4, round_cols<HS_F32, 4>(o + j));
       } else if constexpr (V == 8) {
-        __builtin_nontemporal_store(round_cols<HS_BF16, 8>(o),
-                                    (u32x4v_t *)(row + (int64_t)c * 2));
+        stream_cols(row + (int64_t)c * 2, round_cols<HS_BF16, 8>(o));
       } else {
-        uint2 w;
-        w.x = f32_to_bf16x2(o[0], o[1]);
-        w.y = f32_to_bf16x2(o[2], o[3]);
-        *(uint2 *)(row + (int64_t)c * 2) = w;
+        *(WordsAt<2> *)(row + (int64_t)c * 2) =
+            WordsAt<2>{{f32_to_bf16x2(o[0], o[1]), f32_to_bf16x2(o[2], o[3])}};
       }
     } else {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const int c = col0 + j * 64 + lane;
-        if (c < dim) store_col<OT>(row, c, add ? v[j] + load_col<OT>(row, c) : v[j]);
+        if (c + j >= dim) continue;
+        const float o = v[j] * scale;
+        store_col<OT>(row, c + j, add ? o + load_col<OT>(row, c + j) : o);
       }
     }
   }
 };
 
-template <int DT, int OT, bool WIDE>
+template <int DT, int OT>
 __global__ __launch_bounds__(256) void grad_sums(
     const uint8_t *__restrict__ grad, const uint32_t *__restrict__ tok,
     const uint32_t *__restrict__ pos, int64_t n, int64_t rows, int dim, int places,
@@ -484,7 +466,7 @@ __global__ __launch_bounds__(256) void grad_sums(
     float *__restrict__ part, uint32_t *__restrict__ count, uint32_t *__restrict__ few,
     uint32_t *__restrict__ many, uint8_t *__restrict__ table,
     const uint8_t *__restrict__ present, Zeros z) {
-  using S = Slice<DT, WIDE>;
+  using S = Slice<DT>;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if ((int64_t)blockIdx.x >= sum_blocks) {
     zero_rows(z, present, (int64_t)blockIdx.x - sum_blocks, (int64_t)gridDim.x - sum_blocks);
@@ -493,7 +475,7 @@ __global__ __launch_bounds__(256) void grad_sums(
   const int64_t task = (int64_t)blockIdx.x * 4 + wave;
   if (task >= chunks * slices) return;
   const int64_t c = task / slices;
-  const int col0 = (int)(task - c * slices) * S::kCols;
+  const int slice = (int)(task - c * slices), col = S::column(slice, lane, dim);
   const int64_t lo = c * places;
   const int m = (int)(n - lo < places ? n - lo : places);
   const uint32_t none = (uint32_t)rows;
@@ -512,7 +494,7 @@ __global__ __launch_bounds__(256) void grad_sums(
     for (int u = 0; u < U; ++u) {
       const int i = i0 + u < m ? i0 + u : m - 1;
       const int64_t at = (int64_t)(uint32_t)__builtin_amdgcn_readlane(my_pos, i);
-      S::load(grad + at * gb, col0, lane, dim, v[u]);
+      S::load(grad + at * gb, col, dim, v[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -520,11 +502,9 @@ __global__ __launch_bounds__(256) void grad_sums(
         const uint32_t t = __builtin_amdgcn_readlane(my_tok, i0 + u);
         if (t != cur) {
           if (head) {
-            S::part(part + (c * 2) * dim, col0, lane, dim, acc);
+            S::part(part + (c * 2) * dim, col, dim, acc);
           } else {
-#pragma unroll
-            for (int j = 0; j < S::V; ++j) acc[j] *= scale;
-            S::template write<OT>(table, cur, col0, lane, dim, add, acc);
+            S::template write<OT>(table, cur, col, dim, scale, add, acc);
           }
 #pragma unroll
           for (int j = 0; j < S::V; ++j) acc[j] = 0.0f;
@@ -540,19 +520,17 @@ __global__ __launch_bounds__(256) void grad_sums(
   }
   if (cur == none) return;
   if (head) {
-    S::part(part + (c * 2) * dim, col0, lane, dim, acc);
+    S::part(part + (c * 2) * dim, col, dim, acc);
   } else if (cur == next) {
-    S::part(part + (c * 2 + 1) * dim, col0, lane, dim, acc);
-    if (col0 == 0 && lane == 0) {
+    S::part(part + (c * 2 + 1) * dim, col, dim, acc);
+    if (slice == 0 && lane == 0) {
       const int64_t far = (c + kSpanMany) * places;
       const int l = far < n && tok[far] == cur ? 1 : 0;
       (l ? many : few)[atomicAdd(&count[l], 1u)] = (uint32_t)c;
     }
   } else {
-#pragma unroll
-    for (int j = 0; j < S::V; ++j) acc[j] *= scale;
-    S::template write<OT>(table, cur, col0, lane, dim, add, acc);
-  }
+            S::template write<OT>(table, cur, col, dim, scale, add, acc);
+          }
 }
 
 // Tokens over several chunks: the sum at the end of the chunk where the token begins
@@ -630,9 +608,8 @@ hipError_t launch_sums(const GradWs &w, int side, const void *grad, int64_t n, i
   const int places = chunk_places(n, dim);
   const int64_t chunks = (n + places - 1) / places;
   const int slices = (int)((dim + 64 * V - 1) / (64 * V));
-  const bool wide = dim % V == 0 && ((uintptr_t)grad % 16) == 0 && ((uintptr_t)table % 16) == 0;
   const int64_t sum_blocks = (chunks * slices + 3) / 4;
-  hipLaunchKernelGGL((wide ? grad_sums<DT, OT, true> : grad_sums<DT, OT, false>),
+  hipLaunchKernelGGL((grad_sums<DT, OT>),
                      dim3((unsigned)(sum_blocks + zero_wgs)), dim3(256), 0, st,
                      (const uint8_t *)grad, w.tok[side], w.pos[side], n, rows, (int)dim, places,
                      chunks, slices, sum_blocks, scale, add, w.part, w.count, w.list[0],
@@ -666,8 +643,7 @@ hipError_t launch_embed_grad(const void *grad, int grad_dtype, const void *ids, 
   int side = 0;
   const int elem = table_dtype == HS_F32 ? 4 : 2;
   const int64_t stop = add ? 0 : rows;   // rows of zeros are written below it
-  const int wide = (dim * elem) % 16 == 0 && ((uintptr_t)table % 16) == 0;
-  const Zeros all = {(uint8_t *)table, 0, stop, (int)dim, elem, wide};
+  const Zeros all = {(uint8_t *)table, 0, stop, (int)dim, elem};
   Zeros part[3] = {all, all, all};       // of the second count and scatter, of the sums
   int zero_wgs[3] = {0, 0, 0};
   if (n <= kSmallMax) {

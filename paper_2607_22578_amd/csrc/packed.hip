@@ -29,7 +29,8 @@ namespace {
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kBlock = 256;            // columns per step of a wave
-constexpr int kStageMax = 56 * 1024;   // LDS bytes of staged x
+constexpr int kStageMax = 56 * 1024;     // LDS bytes of staged x, for two workgroups a CU
+constexpr int kLds = 158 * 1024;         // of a CU, for one
 
 __device__ __forceinline__ bf16x8_t decode_codes(uint32_t w) {
   bf16x8_t b;
@@ -86,21 +87,22 @@ constexpr __host__ __device__ int group_of(int h, int j) {
   return (piece * 64 + h * 32) / GROUP;
 }
 
-// How the scales are read: a block's at once (bf16, no columns past the last), or one
-// by one (other tables).  Every load is unconditional, at a clamped place where it
-// would lie outside: with loads under conditions the compiler cannot count those in
-// flight, and waits for the next block's before it multiplies the present one.
-enum ScaleMode { kBf16Whole, kBf16Each, kF32Each };
+// How the scales are read: a block's at once (bf16), in the last block those of the
+// row's last 256 columns, shifted into place, where the row has a part of a block left;
+// or one by one.  Every load is unconditional, at a clamped place where it would lie
+// outside: with loads under conditions the compiler cannot count those in flight, and
+// waits for the next block's before it multiplies the present one.
+enum ScaleMode { kWhole, kTail, kEach };
 
 // The 256 columns of 16 NT table rows, as loaded.
 template <int GROUP, int NT, int MODE>
 struct Block {
   static constexpr int NG = kBlock / GROUP;
-  uint32_t w[NT][2][4];                             // a lane's 64 codes of one row, in halves
-  uint32_t s[NT][MODE == kBf16Whole ? NG / 2 : NG];   // the row's scales, bf16 in pairs
+  uint32_t w[NT][2][4];                         // a lane's 64 codes of one row, in halves
+  uint32_t s[NT][MODE == kEach ? NG : NG / 2];  // the row's scales; bf16 ones in pairs
 
   // kb: block; row, srow: the lane's table rows and their scales; p: its quarter
-  __device__ __forceinline__ void load(int kb, int dim, const uint8_t *const *row,
+  __device__ __forceinline__ void load(int kb, int dim, int scale_bf16, const uint8_t *const *row,
                                        const uint8_t *const *srow, int p) {
     const int c0 = kb * kBlock;
 #pragma unroll
@@ -108,46 +110,64 @@ struct Block {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         int c = c0 + p * 64 + h * 32;
-        if (MODE != kBf16Whole) c = c < dim ? c : 0;
+        if (MODE != kWhole) c = c < dim ? c : 0;
         const u32x4v_t v = *(const u32x4v_t *)(row[t] + c / 2);
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[t][h][j] = v[j];
       }
-    const int g0 = kb * NG;
+    int g0 = kb * NG;
+    if constexpr (MODE == kEach) {
+      if (scale_bf16) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      if constexpr (MODE == kBf16Whole) {
-        __builtin_memcpy(s[t], srow[t] + g0 * 2, NG * 2);   // (aligned to 2 bytes only)
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int g = 0; g < NG; ++g)
+            s[t][g] = (uint32_t)((const uint16_t *)srow[t])[c0 + g * GROUP < dim ? g0 + g : 0]
+                      << 16;
       } else {
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          const int at = c0 + g * GROUP < dim ? g0 + g : 0;
-          s[t][g] = MODE == kF32Each ? ((const uint32_t *)srow[t])[at]
-                                     : ((const uint16_t *)srow[t])[at];
-        }
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int g = 0; g < NG; ++g)
+            s[t][g] = ((const uint32_t *)srow[t])[c0 + g * GROUP < dim ? g0 + g : 0];
+      }
+    } else {
+      if (MODE == kTail && c0 + kBlock > dim) g0 = dim / GROUP - NG;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const WordsAt<NG / 2> v = *(const WordsAt<NG / 2> *)(srow[t] + g0 * 2);
+#pragma unroll
+        for (int i = 0; i < NG / 2; ++i) s[t][i] = v.w[i];
       }
     }
   }
 
-  // Codes of columns past the last become 0 (their scales are finite or not at all
-  // used elsewhere: group scales of the row's first group).
-  __device__ __forceinline__ void clear(int kb, int dim, int p) {
-    if constexpr (MODE != kBf16Whole) {
+  // In a row's last part of a block: codes past the last column become 0, scales move to
+  // their places (those past the last are unused: their sums are 0).
+  __device__ __forceinline__ void trim(int kb, int dim, int p) {
+    if (MODE == kWhole || (kb + 1) * kBlock <= dim) return;
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const bool in = kb * kBlock + p * 64 + h * 32 < dim;
+      for (int h = 0; h < 2; ++h) {
+        const bool in = kb * kBlock + p * 64 + h * 32 < dim;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) w[t][h][j] = in ? w[t][h][j] : 0u;
-        }
+        for (int j = 0; j < 4; ++j) w[t][h][j] = in ? w[t][h][j] : 0u;
+      }
+    if constexpr (MODE == kTail) {
+      for (int n = ((kb + 1) * kBlock - dim) / GROUP; n > 0; --n) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int i = 0; i < NG / 2; ++i)
+            s[t][i] = s[t][i] >> 16 | (i + 1 < NG / 2 ? s[t][i + 1 < NG / 2 ? i + 1 : i] << 16 : 0u);
+      }
     }
   }
 
   __device__ __forceinline__ float scale(int t, int g) const {
-    if constexpr (MODE == kBf16Whole)
-      return __uint_as_float(g & 1 ? s[t][g / 2] & 0xFFFF0000u : s[t][g / 2] << 16);
-    return __uint_as_float(MODE == kBf16Each ? s[t][g] << 16 : s[t][g]);
+    if constexpr (MODE == kEach) return __uint_as_float(s[t][g]);
+    return __uint_as_float(g & 1 ? s[t][g / 2] & 0xFFFF0000u : s[t][g / 2] << 16);
   }
 
   // xs: the lane's MT rows of staged x at the block's first column; xq: bytes between
@@ -251,7 +271,8 @@ __device__ __forceinline__ void stage_x(const uint8_t *x, int64_t m0, int m, int
 // item's first, are in flight while a block is multiplied.
 template <int XT, int GROUP, int MT, int NT, int MODE>
 __global__ __launch_bounds__(256, MT == 1 ? 4 : 2) void score_packed_kernel(
-    const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int64_t rows, int dim,
+    const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int scale_bf16,
+    int64_t rows, int dim,
     const uint8_t *__restrict__ x, int64_t n_x, int ks, int chunk, int64_t row_blocks,
     int64_t items, void *__restrict__ out, int out_f32, int64_t out_stride) {
   constexpr int PARTS = XT == HS_F32 ? 3 : 1;
@@ -264,7 +285,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 4 : 2) void score_packed_kernel(
   const int blocks = (dim + kBlock - 1) / kBlock;
   const int steps = (blocks + ks - 1) / ks, per_chunk = chunk / (ks * kBlock);
   const int row_bytes = chunk * 2 + 16;   // (16 rows' pieces fall on different banks)
-  const int64_t cb = dim / 2, sb = (int64_t)(dim / GROUP) * (MODE == kF32Each ? 4 : 2);
+  const int64_t cb = dim / 2, sb = (int64_t)(dim / GROUP) * (scale_bf16 ? 2 : 4);
 
   // loads run ahead of the sums: (l_item, l_step), with the lane's table rows
   const uint8_t *row[NT], *srow[NT];
@@ -285,7 +306,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 4 : 2) void score_packed_kernel(
   using Blk = Block<GROUP, NT, MODE>;
   auto load = [&](Blk &blk) {
     const int kb = l_step * ks + part_of;
-    blk.load(kb < blocks ? kb : blocks - 1, dim, row, srow, p);
+    blk.load(kb < blocks ? kb : blocks - 1, dim, scale_bf16, row, srow, p);
     if (++l_step == steps) {
       l_step = 0;
       if (l_item + gridDim.x < items) l_item += gridDim.x;   // (past the end: once more)
@@ -331,7 +352,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 4 : 2) void score_packed_kernel(
         xc[m] = xs + (r < mrows ? r : mrows - 1) * row_bytes +
                 (in_chunk * ks + part_of) * kBlock * 2;
       }
-      blk.clear(kb, dim, p);
+      blk.trim(kb, dim, p);
       blk.template add<MT, PARTS>(xc, part_bytes, p, tot);
     }
     if (++step < steps) return;
@@ -400,26 +421,36 @@ hipError_t launch_packed_t(const hs_row_table *t, const void *x, int64_t n_x, vo
   // the columns shared by up to four waves while there are fewer than 4,096 (16 per CU)
   int ks = 1;
   while (ks < 4 && waves * ks < 4096 && t->dim > kBlock * ks) ks *= 2;
-  // x is staged by as many of the ks waves' steps as fit; at least one has to
+  // x is staged whole where that leaves room for more workgroups on a CU or at least one
+  // of them; else by as many of the ks waves' steps as fit, at least one
   const int mrows = (int)(n_x < 16 * MT ? n_x : 16 * MT), parts = XT == HS_F32 ? 3 : 1;
-  const int fit = (kStageMax / (mrows * parts) - 16) / (2 * kBlock);   // blocks
-  while (ks > fit) ks /= 2;
-  const int all = ((int)((t->dim + kBlock - 1) / kBlock) + ks - 1) / ks * ks;
-  const int chunk = (all < fit ? all : fit / ks * ks) * kBlock;
+  const int nb = (int)((t->dim + kBlock - 1) / kBlock);
+  auto staged = [&](int blocks) { return (size_t)mrows * parts * (blocks * kBlock * 2 + 16); };
+  const size_t joined = (size_t)3 * NT * MT * 64 * 16;
+  int wgs = MT == 1 ? 3 : 2, chunk = (nb + ks - 1) / ks * ks;
+  if (staged(chunk) > kStageMax) {
+    if (staged(chunk) + joined <= kLds) {
+      wgs = 1;
+    } else {
+      const int fit = (kStageMax / (mrows * parts) - 16) / (2 * kBlock);   // blocks
+      while (ks > fit) ks /= 2;
+      chunk = fit / ks * ks;
+    }
+  }
   const int64_t per = 16 * NT * (4 / ks), row_blocks = (t->rows + per - 1) / per;
   const int64_t items = row_blocks * mblocks;
-  const size_t lds = (size_t)mrows * parts * (chunk * 2 + 16) +
-                     (ks > 1 ? (size_t)3 * NT * MT * 64 * 16 : 0);
-  auto kernel = t->scale_dtype == HS_F32   ? score_packed_kernel<XT, GROUP, MT, NT, kF32Each>
-                : t->dim % kBlock == 0 ? score_packed_kernel<XT, GROUP, MT, NT, kBf16Whole>
-                                       : score_packed_kernel<XT, GROUP, MT, NT, kBf16Each>;
+  const size_t lds = staged(chunk) + (ks > 1 ? joined : 0);
+  const bool bf16 = t->scale_dtype == HS_BF16;
+  auto kernel = !bf16 || t->dim < kBlock ? score_packed_kernel<XT, GROUP, MT, NT, kEach>
+                : t->dim % kBlock        ? score_packed_kernel<XT, GROUP, MT, NT, kTail>
+                                         : score_packed_kernel<XT, GROUP, MT, NT, kWhole>;
   // (workgroups per CU: 24 rows x 1M x 768 took 105 us with two, 114 with four; one row
   // x 32,000 x 4,096 18 us with three or four, 20 with two)
-  const int64_t grid = (MT == 1 ? 3 : 2) * (int64_t)persistent_grid();
+  const int64_t grid = wgs * (int64_t)persistent_grid();
   hipLaunchKernelGGL(kernel, dim3((unsigned)(items < grid ? items : grid)), dim3(256), lds, st,
-                     (const uint8_t *)t->data, (const uint8_t *)t->scale, t->rows, (int)t->dim,
-                     (const uint8_t *)x, n_x, ks, chunk, row_blocks, items, out,
-                     (int)(out_dtype == HS_F32), out_stride);
+                     (const uint8_t *)t->data, (const uint8_t *)t->scale, (int)bf16, t->rows,
+                     (int)t->dim, (const uint8_t *)x, n_x, ks, chunk * kBlock, row_blocks, items,
+                     out, (int)(out_dtype == HS_F32), out_stride);
   return hipGetLastError();
 }
 

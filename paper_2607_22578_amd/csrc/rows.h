@@ -9,6 +9,13 @@ namespace hs {
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4v_t __attribute__((ext_vector_type(4)));
+// The same with no alignment beyond that of the elements: global accesses need none, so
+// rows of any width and start are read and written 16 bytes at a time.
+typedef uint32_t u32x4e_t __attribute__((ext_vector_type(4), aligned(2)));
+template <int N>
+struct __attribute__((packed)) WordsAt {
+  uint32_t w[N];
+};
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float bf16_to_f32(uint32_t b) { return __uint_as_float(b << 16); }
@@ -23,7 +30,7 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float a) {
   return __builtin_bit_cast(uint16_t, (__bf16)a);
 }
 
-// C (4 or 8) consecutive columns of a row from column `col` (a multiple of C),
+// C (4 or 8) consecutive columns of a row from column `col` (FP4: a multiple of C),
 // undecoded: as loaded, so that several can be in flight.
 template <int DT, int C>
 struct RawCols {
@@ -36,20 +43,13 @@ struct RawCols {
     const uint8_t *p = row + col * kBytes / C;
     if constexpr (kBytes == 2) {
       w[0] = *(const uint16_t *)p;
-    } else if constexpr (kBytes == 4) {
-      w[0] = *(const uint32_t *)p;
-    } else if constexpr (kBytes == 8) {
-      const uint2 v = *(const uint2 *)p;
-      w[0] = v.x;
-      w[1] = v.y;
     } else {
+      constexpr int N = kWords < 4 ? kWords : 4;
 #pragma unroll
-      for (int i = 0; i < kBytes / 16; ++i) {
-        const uint4 v = ((const uint4 *)p)[i];
-        w[4 * i] = v.x;
-        w[4 * i + 1] = v.y;
-        w[4 * i + 2] = v.z;
-        w[4 * i + 3] = v.w;
+      for (int i = 0; i < kWords / N; ++i) {
+        const WordsAt<N> v = ((const WordsAt<N> *)p)[i];
+#pragma unroll
+        for (int j = 0; j < N; ++j) w[N * i + j] = v.w[j];
       }
     }
   }
@@ -94,7 +94,7 @@ struct RawCols {
   }
 };
 
-// One column, for rows whose size or alignment the wide accesses do not fit.
+// One column, for the ends of rows.
 template <int DT>
 __device__ __forceinline__ float load_col(const uint8_t *row, int64_t col) {
   if constexpr (DT == HS_F32) {
@@ -123,6 +123,13 @@ __device__ __forceinline__ u32x4v_t round_cols(const float *v) {
     }
   }
   return o;
+}
+
+__device__ __forceinline__ void store_cols(void *at, u32x4v_t v) { *(u32x4e_t *)at = v; }
+
+// (past the caches: for outputs that the kernel does not read again)
+__device__ __forceinline__ void stream_cols(void *at, u32x4v_t v) {
+  __builtin_nontemporal_store((u32x4e_t)v, (u32x4e_t *)at);
 }
 
 template <int OT>

@@ -1,14 +1,13 @@
 // The k best columns of materialised rows of scores.
 //
-// Phase 1 (rows above 32,768 columns): the largest score of every strip, a thread's
-// columns of a tile; nothing but a stream over the scores.
-// Phase 2: a workgroup per row.  A score that k of the strips' maxima (or of its
-// threads' maxima over them) reach is a lower bound of the k-th best, and a close one
-// while there are many more strips than k; only the strips that reach it are read
-// again, and the few columns in them that reach it are ranked by counting.  Shorter
-// rows are their own maxima.  Where too many columns reach the bound (equal scores) the
-// k-th best score is found bit by bit, and the columns that have it are taken in
-// ascending order.
+// Phase 1 (rows above 32,768 columns): the largest score of every strip of 32 or 64
+// columns, and of every 64 strips; nothing but a stream over the scores.
+// Phase 2: a workgroup per row.  A score that k of those maxima (or of its threads'
+// maxima over them) reach is a lower bound of the k-th best, and a close one while
+// there are many more of them than k; only the strips that reach it are read again, and
+// the few columns in them that reach it are ranked by counting.  Shorter rows are their
+// own maxima.  Where too many columns reach the bound (equal scores) the k-th best
+// score is found bit by bit, and the columns that have it are taken in ascending order.
 // Loops are short on purpose: with one workgroup on a CU, fetching straight-line code
 // took longer than reading the maxima twice (17 against 11 us, 1 x 32,000, k = 50).
 // Floor: the scores, read once.
@@ -19,9 +18,10 @@ namespace hs {
 namespace {
 
 constexpr int kRowCols = 32768;    // longest row done without strips
-constexpr int kStripsMax = 16384;   // strips of a row
 constexpr int kStripThreads = 256;
-constexpr int kLeastReads = 4;     // accesses of a strip, at least
+constexpr int kReads = 8;          // accesses of a strip, 16 bytes each
+constexpr int kSuper = 64;         // strips that share a maximum of the second level: a wave's
+constexpr int kListMax = 4096;     // strips, or groups of them, that reach the bound
 
 // Ordered score; 0 (below every real one) for -inf and NaN, which are never taken.
 __device__ __forceinline__ uint32_t taken_score(float v) {
@@ -68,26 +68,33 @@ __device__ __forceinline__ void visit(const uint8_t *row, const int64_t *col, in
 
 // ---------------------------------------------------------------- strips
 //
-// Strip j = 256 t + i of a row: accesses i, i + 256, ... (`reads` of them) of tile t.
-// 24 rows x 1M fp32: 22 us, 4.3 TB/s.
-template <int DT, bool WIDE>
+// Strip j = 256 t + i of a row: accesses i, i + 256, ... of tile t.  The row's maxima in
+// `maxima`: n1 of strips, then n1 / 64 of groups of 64 strips.
+template <int DT>
 __global__ __launch_bounds__(kStripThreads) void strip_maxima_kernel(
-    const uint8_t *__restrict__ scores, int64_t stride, int64_t n_cols, int reads, int64_t tiles,
+    const uint8_t *__restrict__ scores, int64_t stride, int64_t n_cols, int64_t tiles,
     int64_t items, uint32_t *__restrict__ maxima) {
-  constexpr int ES = DT == HS_F32 ? 4 : 2, C = access_cols<DT, WIDE>(), U = kLeastReads;
+  constexpr int ES = DT == HS_F32 ? 4 : 2, C = access_cols<DT, true>();
+  const int64_t n1 = tiles * kStripThreads, per_row = n1 + n1 / kSuper;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int64_t r = item / tiles, t = item - r * tiles;
     const uint8_t *row = scores + r * stride * ES;
-    const int64_t c0 = t * kStripThreads * C * reads + threadIdx.x * C;
-    float mx = -__builtin_inff();
-    for (int i = 0; i < reads; i += U) {
-      int64_t col[U];
+    int64_t col[kReads];
 #pragma unroll
-      for (int u = 0; u < U; ++u) col[u] = c0 + (int64_t)(i + u) * kStripThreads * C;
-      visit<DT, WIDE, U>(row, col, n_cols,
-                         [&](float v, int64_t) { mx = fmaxf(mx, v); });   // (a NaN loses)
+    for (int i = 0; i < kReads; ++i)
+      col[i] = ((t * kReads + i) * kStripThreads + threadIdx.x) * C;
+    float mx = -__builtin_inff();
+    visit<DT, true, kReads>(row, col, n_cols,
+                            [&](float v, int64_t) { mx = fmaxf(mx, v); });   // (a NaN loses)
+    uint32_t o = taken_score(mx);
+    const int64_t j = t * kStripThreads + threadIdx.x;
+    maxima[r * per_row + j] = o;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t other = __shfl_xor(o, d);
+      o = other > o ? other : o;
     }
-    maxima[item * kStripThreads + threadIdx.x] = taken_score(mx);
+    if ((threadIdx.x & 63) == 0) maxima[r * per_row + n1 + j / kSuper] = o;
   }
 }
 
@@ -129,62 +136,71 @@ __device__ __forceinline__ uint32_t bound_of_maxima(const uint32_t *maxima, int 
   return bound_of<E / 4>(v, k);
 }
 
-// Workgroups of T threads, a row at a time.  STRIPS: the maxima of n_strips strips
-// (a multiple of 256) of 2^reads_log accesses each are in `maxima`.
-template <int DT, bool WIDE, bool STRIPS, int T>
+// Workgroups of T threads, a row at a time.  LEVELS: 0, the row is its own maxima; 1 and
+// 2, the maxima of n1 strips or of n1 / 64 groups of them are searched (n1 is a multiple
+// of 256).
+template <int DT, bool WIDE, int LEVELS, int T>
 __global__ __launch_bounds__(T) void select_rows_kernel(
     const uint8_t *__restrict__ scores, int64_t stride, int64_t n_rows, int64_t n_cols, int k,
-    const uint32_t *__restrict__ maxima, int n_strips, int reads_log, float *__restrict__ out_s,
+    const uint32_t *__restrict__ maxima, int64_t n1, float *__restrict__ out_s,
     int32_t *__restrict__ out_i) {
   constexpr int ES = DT == HS_F32 ? 4 : 2, C = access_cols<DT, WIDE>();
   constexpr int CAP = T * 6;   // (at least k - 1 keys and the 4 T columns of a tie chunk)
   __shared__ uint64_t buf[CAP];
   __shared__ uint32_t group[T];
-  __shared__ uint16_t strip[STRIPS ? kStripsMax : 1];
+  __shared__ uint32_t strip[LEVELS > 0 ? kListMax : 1], super[LEVELS > 1 ? kListMax : 1];
   __shared__ uint32_t bound;
-  __shared__ int count, strips;
+  __shared__ int count, strips, supers;
   const int tid = threadIdx.x, lane = tid & 63;
   for (int64_t r = blockIdx.x; r < n_rows; r += gridDim.x) {
     const uint8_t *row = scores + r * stride * ES;
-    const uint32_t *row_max = maxima + r * n_strips;
-    // f(ordered score, index) for the thread's maxima: those of strips, or the scores
+    const uint32_t *strip_max = maxima + r * (n1 + n1 / kSuper), *super_max = strip_max + n1;
+    // f(ordered score, column) for the thread's columns of the whole row
+    auto each_of_row = [&](auto f) {
+      for (int64_t i = (int64_t)tid * C; i < n_cols; i += 4 * T * C) {
+        const int64_t col[4] = {i, i + T * C, i + 2 * T * C, i + 3 * T * C};
+        visit<DT, WIDE, 4>(row, col, n_cols,
+                           [&](float v, int64_t c) { f(taken_score(v), (uint32_t)c); });
+      }
+    };
+    // f(ordered score, index) for the thread's maxima of the level that is searched
     auto each_max = [&](auto f) {
-      if constexpr (STRIPS) {
-#pragma unroll 4
-        for (int i = tid; i < n_strips / 4; i += T) {
-          const uint4 m = ((const uint4 *)row_max)[i];
-          f(m.x, 4 * i);
-          f(m.y, 4 * i + 1);
-          f(m.z, 4 * i + 2);
-          f(m.w, 4 * i + 3);
-        }
+      if constexpr (LEVELS == 0) {
+        each_of_row(f);
       } else {
-        for (int i = tid * C; i < n_cols; i += 4 * T * C) {
-          const int64_t col[4] = {i, i + T * C, i + 2 * T * C, i + 3 * T * C};
-          visit<DT, WIDE, 4>(row, col, n_cols,
-                             [&](float v, int64_t c) { f(taken_score(v), (int)c); });
+        const uint32_t *m = LEVELS == 1 ? strip_max : super_max;
+        const int64_t n = LEVELS == 1 ? n1 : n1 / kSuper;
+        if (n <= 8 * T) {   // (one by one: as many threads as can have a maximum)
+#pragma unroll 4
+          for (int64_t i = tid; i < n; i += T) f(m[i], (uint32_t)i);
+        } else {
+#pragma unroll 4
+          for (int64_t i = tid; i < n / 4; i += T) {   // (n1 / 64 is a multiple of 4, too)
+            const WordsAt<4> w = ((const WordsAt<4> *)m)[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f(w.w[j], (uint32_t)(4 * i + j));
+          }
         }
       }
     };
     // f(ordered score, column) for the thread's columns that may reach the bound
     auto each_col = [&](auto f) {
-      if constexpr (STRIPS) {
-        const int all = strips << reads_log;
-        for (int i0 = tid; i0 < all; i0 += 4 * T) {
-          int64_t col[4];
+      if (LEVELS == 0 || strips > kListMax) {
+        each_of_row(f);
+        return;
+      }
+      const int all = strips * kReads;
+      for (int i0 = tid; i0 < all; i0 += 4 * T) {
+        int64_t col[4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int i = i0 + u * T;
-            const int j = strip[i < all ? i >> reads_log : 0];
-            const int64_t at = ((int64_t)(j / kStripThreads) << reads_log) +
-                               (i & ((1 << reads_log) - 1));
-            col[u] = i < all ? (at * kStripThreads + j % kStripThreads) * C : n_cols;
-          }
-          visit<DT, WIDE, 4>(row, col, n_cols,
-                             [&](float v, int64_t c) { f(taken_score(v), (uint32_t)c); });
+        for (int u = 0; u < 4; ++u) {
+          const int i = i0 + u * T;
+          const uint32_t j = strip[i < all ? i / kReads : 0];
+          const int64_t at = (int64_t)(j / kStripThreads) * kReads + i % kReads;
+          col[u] = i < all ? (at * kStripThreads + j % kStripThreads) * C : n_cols;
         }
-      } else {
-        each_max([&](uint32_t o, int c) { f(o, (uint32_t)c); });
+        visit<DT, WIDE, 4>(row, col, n_cols,
+                           [&](float v, int64_t c) { f(taken_score(v), (uint32_t)c); });
       }
     };
     // How many of the scores that `each` visits pass f; `count` is left at that.
@@ -201,7 +217,7 @@ __global__ __launch_bounds__(T) void select_rows_kernel(
     uint32_t b = 0u;
     if (k <= T / 4) {
       uint32_t mx = 0u;
-      each_max([&](uint32_t o, int) { mx = o > mx ? o : mx; });
+      each_max([&](uint32_t o, uint32_t) { mx = o > mx ? o : mx; });
       group[tid] = mx;
       __syncthreads();
       if (tid < 64) {
@@ -223,12 +239,32 @@ __global__ __launch_bounds__(T) void select_rows_kernel(
     }
     b = b > 0u ? b : 1u;
     __syncthreads();
-    if (tid == 0) count = strips = 0;
+    if (tid == 0) count = strips = supers = 0;
     __syncthreads();
-    if constexpr (STRIPS) {
-      each_max([&](uint32_t o, int j) {
-        if (o >= b) strip[atomicAdd(&strips, 1)] = (uint16_t)j;
+    auto list = [&](uint32_t *to, int *n, uint32_t j) {
+      const int at = atomicAdd(n, 1);
+      if (at < kListMax) to[at] = j;
+    };
+    if constexpr (LEVELS == 1) {
+      each_max([&](uint32_t o, uint32_t j) {
+        if (o >= b) list(strip, &strips, j);
       });
+      __syncthreads();
+    }
+    if constexpr (LEVELS == 2) {
+      each_max([&](uint32_t o, uint32_t j) {
+        if (o >= b) list(super, &supers, j);
+      });
+      __syncthreads();
+      if (supers > kListMax) {
+        if (tid == 0) strips = kListMax + 1;   // (the whole row)
+      } else {
+#pragma unroll 4
+        for (int i = tid; i < supers * kSuper; i += T) {
+          const uint32_t j = super[i / kSuper] * kSuper + i % kSuper;
+          if (strip_max[j] >= b) list(strip, &strips, j);
+        }
+      }
       __syncthreads();
     }
     each_col([&](uint32_t o, uint32_t c) {
@@ -293,17 +329,8 @@ __global__ __launch_bounds__(T) void select_rows_kernel(
   }
 }
 
-// Accesses of a strip: a power of two, so that a row has at most kStripsMax strips.
-int strip_reads(int64_t n_cols, int cols) {
-  int reads = kLeastReads;
-  while ((n_cols + (int64_t)kStripThreads * cols * reads - 1) /
-             ((int64_t)kStripThreads * cols * reads) * kStripThreads > kStripsMax)
-    reads *= 2;
-  return reads;
-}
-
 int64_t strip_tiles(int64_t n_cols, int cols) {
-  const int64_t tile = (int64_t)kStripThreads * cols * strip_reads(n_cols, cols);
+  const int64_t tile = (int64_t)kStripThreads * cols;
   return (n_cols + tile - 1) / tile;
 }
 
@@ -315,22 +342,29 @@ hipError_t launch_topk_t(const void *scores, int64_t stride, int64_t n_rows, int
   if (n_cols <= kRowCols) {
     // (256 threads do for 4,096 columns while their maxima are four times k)
     if (n_cols <= 4096 && k <= 64)
-      hipLaunchKernelGGL((select_rows_kernel<DT, WIDE, false, 256>), g, dim3(256), 0, st, in,
-                         stride, n_rows, n_cols, k, nullptr, 0, 0, out_s, out_i);
+      hipLaunchKernelGGL((select_rows_kernel<DT, WIDE, 0, 256>), g, dim3(256), 0, st, in,
+                         stride, n_rows, n_cols, k, nullptr, 0, out_s, out_i);
     else
-      hipLaunchKernelGGL((select_rows_kernel<DT, WIDE, false, 1024>), g, dim3(1024), 0, st, in,
-                         stride, n_rows, n_cols, k, nullptr, 0, 0, out_s, out_i);
+      hipLaunchKernelGGL((select_rows_kernel<DT, WIDE, 0, 1024>), g, dim3(1024), 0, st, in,
+                         stride, n_rows, n_cols, k, nullptr, 0, out_s, out_i);
     return hipGetLastError();
   }
-  constexpr int C = access_cols<DT, WIDE>();
-  const int reads = strip_reads(n_cols, C);
-  const int64_t tiles = strip_tiles(n_cols, C), items = n_rows * tiles;
-  hipLaunchKernelGGL((strip_maxima_kernel<DT, WIDE>),
-                     dim3((unsigned)(items < (1 << 20) ? items : (1 << 20))), dim3(kStripThreads),
-                     0, st, in, stride, n_cols, reads, tiles, items, (uint32_t *)ws);
-  hipLaunchKernelGGL((select_rows_kernel<DT, WIDE, true, 1024>), g, dim3(1024), 0, st, in, stride,
-                     n_rows, n_cols, k, (const uint32_t *)ws, (int)(tiles * kStripThreads), __builtin_ctz(reads),
-                     out_s, out_i);
+  if constexpr (WIDE) {   // (rows this long are)
+    const int64_t tiles = strip_tiles(n_cols, access_cols<DT, WIDE>() * kReads);
+    const int64_t items = n_rows * tiles, n1 = tiles * kStripThreads;
+    hipLaunchKernelGGL((strip_maxima_kernel<DT>),
+                       dim3((unsigned)(items < (1 << 20) ? items : (1 << 20))),
+                       dim3(kStripThreads), 0, st, in, stride, n_cols, tiles, items,
+                       (uint32_t *)ws);
+    // (few strips are searched themselves: a step less, and a closer bound; groups of
+    // them while there are four times k: below, their bound would be loose)
+    if (n1 > 32768 && n1 / kSuper >= 4 * (int64_t)k)
+      hipLaunchKernelGGL((select_rows_kernel<DT, WIDE, 2, 1024>), g, dim3(1024), 0, st, in, stride,
+                         n_rows, n_cols, k, (const uint32_t *)ws, n1, out_s, out_i);
+    else
+      hipLaunchKernelGGL((select_rows_kernel<DT, WIDE, 1, 1024>), g, dim3(1024), 0, st, in, stride,
+                         n_rows, n_cols, k, (const uint32_t *)ws, n1, out_s, out_i);
+  }
   return hipGetLastError();
 }
 
@@ -339,9 +373,9 @@ hipError_t launch_topk_t(const void *scores, int64_t stride, int64_t n_rows, int
 size_t topk_rows_workspace_bytes(int64_t n_rows, int64_t n_cols, int k) {
   (void)k;
   if (n_cols <= kRowCols) return 256;
-  int64_t tiles = 0;   // the most over the access widths
-  for (int c : {1, 4, 8}) tiles = tiles > strip_tiles(n_cols, c) ? tiles : strip_tiles(n_cols, c);
-  return (size_t)(n_rows > 0 ? n_rows : 1) * (size_t)tiles * kStripThreads * 4;
+  // (strips of 32 columns; bf16 ones may have 64)
+  const int64_t n1 = strip_tiles(n_cols, 32) * kStripThreads;
+  return (size_t)(n_rows > 0 ? n_rows : 1) * (size_t)(n1 + n1 / kSuper) * 4;
 }
 
 hipError_t launch_topk_rows(const void *scores, int dtype, int64_t stride, int64_t n_rows,
@@ -349,8 +383,7 @@ hipError_t launch_topk_rows(const void *scores, int dtype, int64_t stride, int64
                             hipStream_t st) {
   if (n_rows <= 0) return hipSuccess;
   const int es = dtype == HS_F32 ? 4 : 2;
-  const bool wide = ((uintptr_t)scores % 16) == 0 && n_cols >= 16 / es &&
-                    (n_rows == 1 || stride * es % 16 == 0);
+  const bool wide = n_cols >= 16 / es;
   auto launch = dtype == HS_F32 ? (wide ? launch_topk_t<HS_F32, true> : launch_topk_t<HS_F32, false>)
                                 : (wide ? launch_topk_t<HS_BF16, true>
                                         : launch_topk_t<HS_BF16, false>);

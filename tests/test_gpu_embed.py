@@ -128,7 +128,8 @@ def run_grad(rng, n, rows, dim, din, dout, idt=torch.int32, pad=-1, ids=None, ac
 
 @pytest.mark.parametrize("n,rows,dim", [
     (0, 5, 16), (1, 1, 1), (1, 1000, 8), (63, 7, 24), (64, 513, 40), (65, 511, 33), (129, 3, 520),
-    (1000, 100_000, 16), (4095, 300, 64), (4096, 512, 72), (4097, 513, 72), (5000, 1, 136),
+    (1000, 100_000, 16), (4095, 300, 64), (4096, 512, 72), (4097, 513, 72),
+    (10_240, 700, 20), (10_241, 700, 20), (11_000, 200, 12), (5000, 1, 136),
     (20_011, 50_257, 100), (70_001, 9, 48), (300_000, 40_000, 24)])
 @pytest.mark.parametrize("din,dout", [(F32, F32), (BF16, F32), (BF16, BF16), (F32, BF16)])
 def test_embed_grad_sizes(n, rows, dim, din, dout):

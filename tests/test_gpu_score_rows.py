@@ -244,7 +244,8 @@ def check_topk(scores, k):
 @pytest.mark.parametrize("rows,cols,k", [
     (1, 1, 1), (1, 1, 5), (3, 7, 7), (2, 100, 1024), (1, 4095, 3), (1, 4096, 512), (2, 4097, 513),
     (1, 32_000, 50), (5, 50_257, 1), (700, 333, 20), (70, 9001, 100), (2, 100_003, 1024),
-    (24, 250_000, 100), (1, 1_000_003, 64)])
+    (24, 250_000, 100), (1, 1_000_003, 64),
+    (5, 72_232, 9), (2, 3_000_001, 300), (1, 6_000_000, 5), (1, 40_000, 1024), (3, 33_001, 256)])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_topk_sizes(rows, cols, k, dtype):
     rng = np.random.default_rng(rows + cols + k)
