@@ -433,8 +433,8 @@ hs_status hs_pack_rows(const void *src, int32_t src_dtype, int64_t rows, int64_t
  * scaled in fp32 and rounded once to out_dtype.  Ids outside [0, rows) and ids
  * equal to pad_id (-1: no such id) stand for no token: their rows are zeros.
  *   ids      [n] int32 (ids_is_i64 = 0) or int64 (= 1) device, 0 <= n <= 2^30
- *   out      [n x dim] device out, HS_F32 or HS_BF16, aligned to its element
- *            (16-byte rows use 128-bit accesses) */
+ *   out      [n x dim] device out, HS_F32 or HS_BF16, aligned to its element; must
+ *            not overlap the table */
 hs_status hs_embed(const hs_row_table *table, const void *ids, int32_t ids_is_i64, int64_t n,
                    float scale, int64_t pad_id, void *out, int32_t out_dtype, void *stream);
 
@@ -447,9 +447,9 @@ hs_status hs_embed(const hs_row_table *table, const void *ids, int32_t ids_is_i6
  * (accumulate = 1: are left untouched).
  *   d_out    [n x dim] device, HS_F32 or HS_BF16
  *   d_table  [rows x dim] device, HS_F32 or HS_BF16: out (accumulate = 0) or in and
- *            out (1).  Both aligned to their elements (16-byte aligned rows use
- *            128-bit accesses)
- *   ws       device, 256-byte aligned, of hs_embed_grad_bytes' size */
+ *            out (1).  Both aligned to their elements; must not overlap
+ *   ws       device, 256-byte aligned, of hs_embed_grad_bytes' size; every call writes
+ *            what it reads of it, so calls may share one unless they overlap in time */
 hs_status hs_embed_grad_bytes(int64_t n, int64_t rows, int64_t dim, size_t *bytes);
 hs_status hs_embed_grad(const void *d_out, int32_t d_out_dtype, const void *ids,
                         int32_t ids_is_i64, int64_t n, int64_t rows, int64_t dim, float scale,
@@ -463,10 +463,11 @@ hs_status hs_embed_grad(const void *d_out, int32_t d_out_dtype, const void *ids,
  * out_dtype.  Equal table rows get bit-identical scores.
  *   table      an HS_FP4_E2M1 table
  *   x          [n_x x dim] device, HS_F32 or HS_BF16, 16-byte aligned; 0 <= n_x <= 2^20
- *              (finite: a NaN or infinity in row m makes out[m] NaN)
+ *              (finite: a NaN or infinity in row m makes out[m] NaN or infinite)
  *   out        [n_x x out_stride] device out, HS_F32 or HS_BF16, out_stride >= rows
- *              elements; columns [rows, out_stride) are left as they were
- * Tables are read once for up to 64 rows of x. */
+ *              elements; columns [rows, out_stride) are left as they were; must not
+ *              overlap the table or x
+ * The table is read once for every 64 rows of x (fp32: 32). */
 hs_status hs_score_packed(const hs_row_table *table, const void *x, int32_t x_dtype, int64_t n_x,
                           void *out, int32_t out_dtype, int64_t out_stride, void *stream);
 
@@ -518,8 +519,10 @@ hs_status hs_adjust_scores(const hs_adjust *adjust, const void *scores, int64_t 
  *   k           1 <= k <= 1024 (k > n_cols pads)
  *   topk_score  [n_rows x k] fp32 device out
  *   topk_index  [n_rows x k] int32 device out
- *   ws          device, 256-byte aligned, of hs_topk_rows_bytes' size
- * Bit-exact and deterministic. */
+ *   ws          device, 256-byte aligned, of hs_topk_rows_bytes' size; every call
+ *               writes what it reads of it
+ * Bit-exact and deterministic.  (Rows with thousands of scores equal to the k-th best
+ * take several passes over them.) */
 hs_status hs_topk_rows_bytes(int64_t n_rows, int64_t n_cols, int32_t k, size_t *bytes);
 hs_status hs_topk_rows(const void *scores, int32_t dtype, int64_t stride, int64_t n_rows,
                        int64_t n_cols, int32_t k, float *topk_score, int32_t *topk_index,

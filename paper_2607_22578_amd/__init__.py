@@ -577,9 +577,8 @@ class MergedRetrieval:
     # ------------------------------------------------ packed 4-bit corpus
 
     def enable_packed(self, batch: int = 64):
-        """Allocates the scores, masks and workspace of run_packed: `batch` distinct
-        queries are scored at a time, [batch x n_corpus] fp32 scores (rows padded to
-        128 bytes)."""
+        """Allocates the scores and workspace of run_packed: `batch` distinct queries are
+        scored at a time, [batch x n_corpus] fp32 scores (rows padded to 128 bytes)."""
         import torch
         if batch < 1:
             raise ValueError("batch must be at least 1")
@@ -588,8 +587,7 @@ class MergedRetrieval:
         self.packed_stride = max((self.N + 31) // 32 * 32, 32)
         self.packed_scores = torch.empty((self.packed_batch, self.packed_stride),
                                          dtype=torch.float32, device=dev)
-        self.packed_allow = torch.empty((max(self.R, 1), max((self.N + 31) // 32, 1)),
-                                        dtype=torch.int32, device=dev)
+        self.packed_allow = None   # (made for the first masks per request)
         self.packed_ws = torch.empty(hs_topk_rows_bytes(self.packed_batch, self.N, self.k),
                                      dtype=torch.uint8, device=dev)
 
@@ -619,8 +617,10 @@ class MergedRetrieval:
             _tensor(allow, "allow", self.ws.device, dtypes=(_torch.int32,))
             adj.allow = _ptr(allow)
             if allow.dim() == 2:
-                hs_scatter(allow, self.R, words * 4, self.first_index, 0, self.R, self.n_unique,
-                           self.packed_allow, stream=stream)
+                if self.packed_allow is None:
+                    self.packed_allow = _torch.empty((self.packed_batch, words),
+                                                     dtype=_torch.int32, device=self.ws.device)
+                adj.allow = _ptr(self.packed_allow)
                 adj.allow_stride = words
         for b0 in range(0, nu, self.packed_batch):
             nb = min(self.packed_batch, nu - b0)
@@ -629,7 +629,8 @@ class MergedRetrieval:
                             self.packed_stride, stream=stream)
             if adj.allow:
                 if adj.allow_stride:
-                    adj.allow = self.packed_allow.data_ptr() + b0 * words * 4
+                    hs_scatter(allow, self.R, words * 4, self.first_index.data_ptr() + b0 * 4, 0,
+                               nb, None, self.packed_allow, stream=stream)
                 hs_adjust_scores(adj, self.packed_scores, self.packed_stride, self.packed_scores,
                                  self.packed_stride, HS_F32, nb, self.N, stream=stream)
             hs_topk_rows(self.packed_scores, HS_F32, self.packed_stride, nb, self.N, self.k,

@@ -131,12 +131,6 @@ __device__ __forceinline__ uint32_t token_key(const void *ids, int is64, int64_t
   return (uint32_t)(id >= 0 && id < rows && id != pad ? id : rows);
 }
 
-// Orders a wave's LDS accesses (its lanes run together: only the compiler has to).
-__device__ __forceinline__ void wave_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // Lanes of the wave with the same digit as this one, among the lanes in `in`.
 __device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, bool in) {
   uint64_t m = __builtin_amdgcn_ballot_w64(in);

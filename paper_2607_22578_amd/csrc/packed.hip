@@ -16,8 +16,8 @@
 // the quarters (swaps of halves, then of quarters; for groups of 128 columns halves
 // alone), and x, staged in LDS, is read in the same order.
 // Floor: the table, read once.  24 bf16 rows x 1M x 768, group 64 (504 MB): 105 us, 4.8
-// TB/s; one row x 32,000 x 4,096, group 32 (74 MB): 18 us, 4.1 TB/s (a plain copy of that
-// size reads at 6).
+// TB/s; one row x 32,000 x 4,096, group 32 (74 MB): 16.5 us, 4.5 TB/s (a plain read of that
+// size runs at 6).
 #include "rows.h"
 
 namespace hs {
@@ -143,7 +143,7 @@ struct Block {
   }
 
   // In a row's last part of a block: codes past the last column become 0, scales move to
-  // their places (those past the last are unused: their sums are 0).
+  // their places and become 0 past the last.
   __device__ __forceinline__ void trim(int kb, int dim, int p) {
     if (MODE == kWhole || (kb + 1) * kBlock <= dim) return;
 #pragma unroll
@@ -154,7 +154,12 @@ struct Block {
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[t][h][j] = in ? w[t][h][j] : 0u;
       }
-    if constexpr (MODE == kTail) {
+    if constexpr (MODE == kEach) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) s[t][g] = kb * kBlock + g * GROUP < dim ? s[t][g] : 0u;
+    } else {
       for (int n = ((kb + 1) * kBlock - dim) / GROUP; n > 0; --n) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)

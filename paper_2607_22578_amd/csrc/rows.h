@@ -146,6 +146,12 @@ __device__ __forceinline__ int64_t row_bytes(int64_t dim) {
   return DT == HS_F32 ? dim * 4 : DT == HS_BF16 ? dim * 2 : DT == HS_FP8_E4M3 ? dim : dim / 2;
 }
 
+// Orders a wave's LDS accesses (its lanes run together: only the compiler has to).
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 __device__ __forceinline__ int64_t load_id(const void *ids, int is64, int64_t i) {
   return is64 ? ((const int64_t *)ids)[i] : (int64_t)((const int32_t *)ids)[i];
 }

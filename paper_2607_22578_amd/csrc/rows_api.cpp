@@ -99,6 +99,16 @@ static uint64_t table_bytes(const hs_row_table *t) {
          : t->dtype == HS_FP8_E4M3 ? cells : cells / 2;
 }
 
+// Whether out[bytes] overlaps the table's rows or scales.
+static bool on_table(const hs_row_table *t, const void *out, uint64_t bytes) {
+  const uint64_t rows = (uint64_t)t->rows;
+  const uint64_t scales = t->dtype == HS_FP8_E4M3 ? rows * 4
+                          : t->dtype == HS_FP4_E2M1
+                              ? rows * (uint64_t)(t->dim / t->group) * elem(t->scale_dtype)
+                              : 0;
+  return overlap(t->data, table_bytes(t), out, bytes) || overlap(t->scale, scales, out, bytes);
+}
+
 static hs_status check_ids(const void *ids, int32_t is64, int64_t n, const char *who) {
   if (n < 0 || n > kIdsMax)
     return fail(HS_ERR_INVALID_ARG, "%s: n %lld out of [0, 2^30]", who, (long long)n);
@@ -152,8 +162,7 @@ hs_status hs_embed(const hs_row_table *table, const void *ids, int32_t ids_is_i6
     return fail(HS_ERR_UNSUPPORTED, "%s: out_dtype %d unsupported", who, out_dtype);
   if (n > 0 && !out) return fail(HS_ERR_INVALID_ARG, "%s: null out", who);
   if (!aligned(out, elem(out_dtype))) return fail(HS_ERR_ALIGNMENT, "%s: misaligned out", who);
-  if (overlap(table->data, table_bytes(table), out,
-              (uint64_t)n * (uint64_t)table->dim * elem(out_dtype)))
+  if (on_table(table, out, (uint64_t)n * (uint64_t)table->dim * elem(out_dtype)))
     return fail(HS_ERR_INVALID_ARG, "%s: table and out overlap", who);
   return device_status(hs::launch_embed(table, ids, ids_is_i64, n, scale, pad_id, out, out_dtype,
                                         (hipStream_t)stream),
@@ -224,7 +233,7 @@ hs_status hs_score_packed(const hs_row_table *table, const void *x, int32_t x_dt
   if (n_x > 0 && table->rows > 0) {
     const uint64_t ob = ((uint64_t)(n_x - 1) * (uint64_t)out_stride + (uint64_t)table->rows) *
                         elem(out_dtype);
-    if (overlap(table->data, table_bytes(table), out, ob) ||
+    if (on_table(table, out, ob) ||
         overlap(x, (uint64_t)n_x * (uint64_t)table->dim * elem(x_dtype), out, ob))
       return fail(HS_ERR_INVALID_ARG, "%s: out overlaps the table or x", who);
   }

@@ -10,7 +10,9 @@
 // score is found bit by bit, and the columns that have it are taken in ascending order.
 // Loops are short on purpose: with one workgroup on a CU, fetching straight-line code
 // took longer than reading the maxima twice (17 against 11 us, 1 x 32,000, k = 50).
-// Floor: the scores, read once.
+// Floor: the scores, read once.  24 x 1M fp32, k = 100 (96 MB): 17 us for the strips, 5.6
+// TB/s, and 12 for the selection, which is latency: 24 workgroups, a few dependent
+// passes.  1 x 32,000, k = 50: 10 us.
 #include "rows.h"
 
 namespace hs {
@@ -145,7 +147,7 @@ __global__ __launch_bounds__(T) void select_rows_kernel(
     const uint32_t *__restrict__ maxima, int64_t n1, float *__restrict__ out_s,
     int32_t *__restrict__ out_i) {
   constexpr int ES = DT == HS_F32 ? 4 : 2, C = access_cols<DT, WIDE>();
-  constexpr int CAP = T * 6;   // (at least k - 1 keys and the 4 T columns of a tie chunk)
+  constexpr int CAP = T * 6;   // (at least k - 1 keys and T columns of a tie)
   __shared__ uint64_t buf[CAP];
   __shared__ uint32_t group[T];
   __shared__ uint32_t strip[LEVELS > 0 ? kListMax : 1], super[LEVELS > 1 ? kListMax : 1];
@@ -238,45 +240,54 @@ __global__ __launch_bounds__(T) void select_rows_kernel(
       }
     }
     b = b > 0u ? b : 1u;
-    __syncthreads();
-    if (tid == 0) count = strips = supers = 0;
-    __syncthreads();
-    auto list = [&](uint32_t *to, int *n, uint32_t j) {
-      const int at = atomicAdd(n, 1);
-      if (at < kListMax) to[at] = j;
-    };
-    if constexpr (LEVELS == 1) {
-      each_max([&](uint32_t o, uint32_t j) {
-        if (o >= b) list(strip, &strips, j);
-      });
+    // lists the strips that reach `least`
+    auto gather = [&](uint32_t least) {
       __syncthreads();
-    }
-    if constexpr (LEVELS == 2) {
-      each_max([&](uint32_t o, uint32_t j) {
-        if (o >= b) list(super, &supers, j);
-      });
+      if (tid == 0) count = strips = supers = 0;
       __syncthreads();
-      if (supers > kListMax) {
-        if (tid == 0) strips = kListMax + 1;   // (the whole row)
-      } else {
+      auto list = [&](uint32_t *to, int *n, uint32_t j) {
+        const int at = atomicAdd(n, 1);
+        if (at < kListMax) to[at] = j;
+      };
+      if constexpr (LEVELS == 1) {
+        each_max([&](uint32_t o, uint32_t j) {
+          if (o >= least) list(strip, &strips, j);
+        });
+        __syncthreads();
+      }
+      if constexpr (LEVELS == 2) {
+        each_max([&](uint32_t o, uint32_t j) {
+          if (o >= least) list(super, &supers, j);
+        });
+        __syncthreads();
+        if (supers > kListMax) {
+          if (tid == 0) strips = kListMax + 1;   // (the whole row)
+        } else {
 #pragma unroll 4
-        for (int i = tid; i < supers * kSuper; i += T) {
-          const uint32_t j = super[i / kSuper] * kSuper + i % kSuper;
-          if (strip_max[j] >= b) list(strip, &strips, j);
+          for (int i = tid; i < supers * kSuper; i += T) {
+            const uint32_t j = super[i / kSuper] * kSuper + i % kSuper;
+            if (strip_max[j] >= least) list(strip, &strips, j);
+          }
         }
+        __syncthreads();
       }
+    };
+    gather(b);
+    int m = CAP + 1;   // (more strips than the list holds: too many columns)
+    if (LEVELS == 0 || strips <= kListMax) {
+      each_col([&](uint32_t o, uint32_t c) {
+        if (o >= b) {
+          const int at = atomicAdd(&count, 1);
+          if (at < CAP) buf[at] = (uint64_t)o << 32 | ~c;
+        }
+      });
       __syncthreads();
+      m = count;
     }
-    each_col([&](uint32_t o, uint32_t c) {
-      if (o >= b) {
-        const int at = atomicAdd(&count, 1);
-        if (at < CAP) buf[at] = (uint64_t)o << 32 | ~c;
-      }
-    });
-    __syncthreads();
-    int m = count;
-    if (m > CAP) {
-      // t: the k-th best score; often the bound itself (equal scores)
+    if (m > CAP || m > 2 * k + 512) {   // (or too many to rank: it takes m^2 reads)
+      // t: the k-th best score; often the bound itself (equal scores).  Those above it are
+      // in few strips.
+      gather(b + 1u);
       uint32_t t = b;
       int above = tally(each_col, [&](uint32_t o) { return o > t; });
       if (above >= k) {
@@ -296,14 +307,19 @@ __global__ __launch_bounds__(T) void select_rows_kernel(
       __syncthreads();
       // columns of score t, in ascending chunks, until there are k keys
       for (int64_t c0 = 0; c0 < n_cols && count < k; c0 += 4 * T) {
-        __syncthreads();   // (everyone has seen the count)
+        bool tie[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int64_t c = c0 + u * T + tid;
-          if (c < n_cols && taken_score(load_col<DT>(row, c)) == t)
-            buf[atomicAdd(&count, 1)] = (uint64_t)t << 32 | ~(uint32_t)c;
+          tie[u] = c < n_cols && taken_score(load_col<DT>(row, c)) == t;
         }
-        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {   // (T columns at a time: few more than needed)
+          __syncthreads();              // (everyone has seen the count)
+          if (tie[u]) buf[atomicAdd(&count, 1)] = (uint64_t)t << 32 | ~(uint32_t)(c0 + u * T + tid);
+          __syncthreads();
+          if (count >= k) break;
+        }
       }
       m = count;
     }

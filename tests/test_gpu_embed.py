@@ -170,6 +170,23 @@ def test_embed_grad_wide_keys():
             assert (out.double() - want).abs().max() <= (cnt + 2) * 2.0 ** -24 * cnt * 6
 
 
+def test_embed_grad_offsets_past_32_bits():
+    """More than 4 GiB of gradients, and of table: chosen rows and columns."""
+    n, dim, rows = 280_000, 8192, 300_000
+    dev = device()
+    d = torch.zeros(n, dim, dtype=BF16, device=dev)
+    ids = torch.arange(n, device=dev) + 7
+    ids[-1000:] = rows - 1
+    d[-1000:] = 1.0
+    d[5] = 2.0
+    d[-1001] = 3.0
+    out = hs.embed_grad(d, ids, rows)
+    assert torch.all(out[rows - 1] == 1000.0) and torch.all(out[12] == 2.0)
+    assert torch.all(out[n - 1001 + 7] == 3.0)
+    assert out[:7].abs().max().item() == 0 and out[n + 7:rows - 1].abs().max().item() == 0
+    assert out[13:n - 1001 + 7].abs().max().item() == 0
+
+
 def test_embed_grad_repeats_bit_for_bit_and_unaligned():
     rng = np.random.default_rng(4)
     d, ids, out = run_grad(rng, 50_000, 900, 72, BF16, F32)

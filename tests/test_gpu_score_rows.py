@@ -271,6 +271,47 @@ def test_topk_hard_orders(k):
     check_topk(torch.from_numpy(s).to(device()), k)
 
 
+@pytest.mark.parametrize("cols,k", [(300_000, 20), (9_000_000, 20), (2_000_000, 700)])
+def test_topk_long_rows_of_equal_scores(cols, k):
+    """More strips, and groups of them, with the k-th best score than their lists hold."""
+    s = torch.zeros(2, cols, device=device())
+    s[1, ::3] = 1.0
+    s[1, cols - 5] = 2.0
+    s[0, 1000:] = -1.0
+    got_s, got_i = hs.topk_rows(s, k)
+    assert got_i[0].tolist() == list(range(k)) and torch.all(got_s[0] == 0)
+    first = [cols - 5] + [3 * i for i in range(k)]
+    assert got_i[1].tolist() == first[:k]
+    assert got_s[1].tolist() == [2.0] + [1.0] * (k - 1)
+
+
+def test_long_rows_past_32_bits():
+    """A row of more than 4 GiB, and rows that start past it."""
+    dev = device()
+    cols = 2 ** 31 - 1
+    s = torch.full((1, cols), -2.0, dtype=BF16, device=dev)
+    at = [3, 2 ** 30 + 11, 2 ** 31 - 2]
+    s[0, at[0]], s[0, at[1]], s[0, at[2]] = 1.0, 3.0, 2.0
+    got_s, got_i = hs.topk_rows(s, 3)
+    assert got_i[0].tolist() == [at[1], at[2], at[0]] and got_s[0].tolist() == [3.0, 2.0, 1.0]
+    ids = torch.tensor([at[2], 5], dtype=torch.int32, device=dev)
+    off = torch.tensor([0, 2], dtype=torch.int64, device=dev)
+    one = torch.ones(1, device=dev)
+    hs.adjust_scores(s, seen=ids, seen_off=off, presence=one, out=s)
+    assert s[0, at[2]].item() == 1.0 and s[0, 5].item() == -3.0 and s[0, 6].item() == -2.0
+    s = s.view(-1)[:2 ** 31 - 32768].view(-1, 32768)     # 65,535 rows
+    rows = s.shape[0]
+    s.fill_(0.5)
+    s[rows - 1, 77] = 9.0
+    off = torch.zeros(rows + 1, dtype=torch.int64, device=dev)
+    off[-1] = 1
+    hs.adjust_scores(s, bias_id=torch.tensor([4], dtype=torch.int32, device=dev), bias=one,
+                     bias_off=off, out=s)
+    assert s[rows - 1, 4].item() == 1.5 and s[rows - 2, 4].item() == 0.5
+    got_s, got_i = hs.topk_rows(s, 2)
+    assert got_i[rows - 1].tolist() == [77, 4] and got_i[rows - 2].tolist() == [0, 1]
+
+
 def test_topk_strides_and_many_rows():
     rng = np.random.default_rng(2)
     buf = torch.from_numpy(rng.standard_normal((40, 5003)).astype(np.float32)).to(device())

@@ -57,7 +57,8 @@ def test_embed():
                           (3, -1, INVALID), (3, 2 ** 30 + 1, INVALID),
                           (4, float("nan"), INVALID), (4, float("inf"), INVALID),
                           (6, None, INVALID), (6, 2 * BIG + 2, ALIGN), (7, hs.HS_FP8_E4M3, UNSUP),
-                          (6, FAKE + 64, INVALID)]:      # inside the table
+                          (6, FAKE + 64, INVALID),       # inside the table
+                          (6, BIG + 64, INVALID)]:       # inside its scales
         args = list(good)
         args[at] = bad
         refused(code, hs.hs_embed, *args)
