@@ -434,7 +434,7 @@ hs_status hs_pack_rows(const void *src, int32_t src_dtype, int64_t rows, int64_t
  * equal to pad_id (-1: no such id) stand for no token: their rows are zeros.
  *   ids      [n] int32 (ids_is_i64 = 0) or int64 (= 1) device, 0 <= n <= 2^30
  *   out      [n x dim] device out, HS_F32 or HS_BF16, aligned to its element; must
- *            not overlap the table */
+ *            not overlap the table or ids */
 hs_status hs_embed(const hs_row_table *table, const void *ids, int32_t ids_is_i64, int64_t n,
                    float scale, int64_t pad_id, void *out, int32_t out_dtype, void *stream);
 
@@ -518,7 +518,7 @@ hs_status hs_adjust_scores(const hs_adjust *adjust, const void *scores, int64_t 
  *               stride >= n_cols elements; 0 <= n_rows <= 2^20, 0 <= n_cols <= 2^31 - 1
  *   k           1 <= k <= 1024 (k > n_cols pads)
  *   topk_score  [n_rows x k] fp32 device out
- *   topk_index  [n_rows x k] int32 device out
+ *   topk_index  [n_rows x k] int32 device out; neither overlaps scores or the other
  *   ws          device, 256-byte aligned, of hs_topk_rows_bytes' size; every call
  *               writes what it reads of it
  * Bit-exact and deterministic.  (Rows with thousands of scores equal to the k-th best

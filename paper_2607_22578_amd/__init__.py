@@ -605,7 +605,13 @@ class MergedRetrieval:
                              f"{self.N} x {self.d}")
         if not hasattr(self, "packed_scores"):
             self.enable_packed()
+            # (`stream` must not overtake what still uses the memory just taken)
+            _torch.cuda.current_stream(self.ws.device).synchronize()
         words = (self.N + 31) // 32
+        if allow is not None and allow.dim() == 2 and self.packed_allow is None:
+            self.packed_allow = _torch.empty((self.packed_batch, max(words, 1)),
+                                             dtype=_torch.int32, device=self.ws.device)
+            _torch.cuda.current_stream(self.ws.device).synchronize()
         nu = self.dedup(keys, stream, host_count=True)
         hs_scatter(q_req, self.R, self.q_row_bytes, self.first_index, 0, self.R, self.n_unique,
                    self.q_unique, stream=stream)
@@ -617,9 +623,6 @@ class MergedRetrieval:
             _tensor(allow, "allow", self.ws.device, dtypes=(_torch.int32,))
             adj.allow = _ptr(allow)
             if allow.dim() == 2:
-                if self.packed_allow is None:
-                    self.packed_allow = _torch.empty((self.packed_batch, words),
-                                                     dtype=_torch.int32, device=self.ws.device)
                 adj.allow = _ptr(self.packed_allow)
                 adj.allow_stride = words
         for b0 in range(0, nu, self.packed_batch):

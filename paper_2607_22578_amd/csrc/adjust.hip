@@ -95,12 +95,14 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(
       s1 = a.seen_off[r + 1];
       s0 = s0 < 0 ? 0 : s0;
       s1 = s1 > a.n_seen ? a.n_seen : s1;
+      s0 = s0 > s1 ? s1 : s0;   // (entries are counted on from here: no overflow)
     }
     if (a.bias_off) {
       b0 = a.bias_off[r];
       b1 = a.bias_off[r + 1];
       b0 = b0 < 0 ? 0 : b0;
       b1 = b1 > a.n_bias ? a.n_bias : b1;
+      b0 = b0 > b1 ? b1 : b0;
     }
     const bool lists = s0 < s1 || b0 < b1;
     const int64_t late = s0 + (a.prompt_len ? a.prompt_len[r] : 0);

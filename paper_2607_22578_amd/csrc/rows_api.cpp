@@ -162,8 +162,9 @@ hs_status hs_embed(const hs_row_table *table, const void *ids, int32_t ids_is_i6
     return fail(HS_ERR_UNSUPPORTED, "%s: out_dtype %d unsupported", who, out_dtype);
   if (n > 0 && !out) return fail(HS_ERR_INVALID_ARG, "%s: null out", who);
   if (!aligned(out, elem(out_dtype))) return fail(HS_ERR_ALIGNMENT, "%s: misaligned out", who);
-  if (on_table(table, out, (uint64_t)n * (uint64_t)table->dim * elem(out_dtype)))
-    return fail(HS_ERR_INVALID_ARG, "%s: table and out overlap", who);
+  const uint64_t ob = (uint64_t)n * (uint64_t)table->dim * elem(out_dtype);
+  if (on_table(table, out, ob) || overlap(ids, (uint64_t)n * (ids_is_i64 ? 8 : 4), out, ob))
+    return fail(HS_ERR_INVALID_ARG, "%s: out overlaps the table or ids", who);
   return device_status(hs::launch_embed(table, ids, ids_is_i64, n, scale, pad_id, out, out_dtype,
                                         (hipStream_t)stream),
                        "hs_embed launch");
@@ -324,6 +325,14 @@ hs_status hs_topk_rows(const void *scores, int32_t dtype, int64_t stride, int64_
     return fail(HS_ERR_INVALID_ARG, "%s: null output", who);
   if (!aligned(topk_score, 4) || !aligned(topk_index, 4))
     return fail(HS_ERR_ALIGNMENT, "%s: misaligned output", who);
+  if (n_rows > 0 && n_cols > 0) {
+    const uint64_t sb = ((uint64_t)(n_rows - 1) * (uint64_t)stride + (uint64_t)n_cols) *
+                        elem(dtype),
+                   kb = (uint64_t)n_rows * (uint64_t)k * 4;
+    if (overlap(scores, sb, topk_score, kb) || overlap(scores, sb, topk_index, kb) ||
+        overlap(topk_score, kb, topk_index, kb))
+      return fail(HS_ERR_INVALID_ARG, "%s: scores and the outputs overlap", who);
+  }
   const size_t need = hs::topk_rows_workspace_bytes(n_rows, n_cols, k);
   if (!ws || ws_bytes < need)
     return fail(HS_ERR_WORKSPACE, "%s: workspace %zu bytes, need %zu", who, ws_bytes, need);

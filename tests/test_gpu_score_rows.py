@@ -230,6 +230,15 @@ def test_adjust_offsets_are_clamped():
     want = torch.zeros(4, 64)
     want[0, 1] = want[2, 1] = want[2, 2] = want[3, 3] = -1.0
     assert torch.equal(got, want)
+    # the ends of int64, for both lists: the second row has all of them
+    lo, hi = -2 ** 63, 2 ** 63 - 1
+    off = torch.tensor([hi, lo, hi, hi, lo], dtype=torch.int64, device=dev)
+    got = hs.adjust_scores(s, seen=seen, seen_off=off, presence=torch.ones(4, device=dev),
+                           bias_id=seen, bias=torch.full((3,), 0.25, device=dev),
+                           bias_off=off).cpu()
+    want = torch.zeros(4, 64)
+    want[1, 1:4] = -0.75
+    assert torch.equal(got, want)
 
 
 # ------------------------------------------------------------------ top-k

@@ -58,6 +58,7 @@ def test_embed():
                           (4, float("nan"), INVALID), (4, float("inf"), INVALID),
                           (6, None, INVALID), (6, 2 * BIG + 2, ALIGN), (7, hs.HS_FP8_E4M3, UNSUP),
                           (6, FAKE + 64, INVALID),       # inside the table
+                          (1, 2 * BIG + 64, INVALID),    # ids inside out
                           (6, BIG + 64, INVALID)]:       # inside its scales
         args = list(good)
         args[at] = bad
@@ -163,7 +164,10 @@ def test_topk_rows():
                           (2, 99_999, INVALID), (3, -1, INVALID), (4, -1, INVALID),
                           (5, 0, INVALID), (5, 1025, INVALID), (6, None, INVALID),
                           (6, BIG + 2, ALIGN), (7, None, INVALID), (7, 2 * BIG + 1, ALIGN),
-                          (8, None, WS), (8, 3 * BIG + 16, ALIGN), (9, need - 1, WS)]:
+                          (8, None, WS), (8, 3 * BIG + 16, ALIGN), (9, need - 1, WS),
+                          # outputs on the scores' last column, or on each other's
+                          (6, FAKE + 4 * 400_000 - 4, INVALID), (7, FAKE, INVALID),
+                          (7, BIG + 4 * 4 * 50 - 4, INVALID)]:
         args = list(good)
         args[at] = bad
         refused(code, hs.hs_topk_rows, *args)
