@@ -90,20 +90,28 @@ struct Zeros {
 };
 
 // Zeros for the absent ones among rows r0 .. r0 + 3: a set bit each in `absent`.
+// Neighbours are written as one span, a wave's accesses at multiples of 1 KiB, so rows of
+// any width fill whole cache lines but for the span's ends.
 __device__ __forceinline__ void zero_four(const Zeros &z, int64_t r0, uint32_t absent) {
-  const int lane = threadIdx.x & 63;
-  const int vecs = z.dim * z.elem / 16, rest = z.dim * z.elem % 16 / z.elem;
+  const int64_t rb = (int64_t)z.dim * z.elem;
   const u32x4v_t zero = {0u, 0u, 0u, 0u};
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    if (!((absent >> r) & 1u)) continue;
-    uint8_t *row = z.table + (r0 + r) * z.dim * z.elem;
-    for (int i = lane; i < vecs; i += 64) stream_cols(row + i * 16, zero);
-    if (lane < rest) {
-      if (z.elem == 4)
-        ((uint32_t *)row)[vecs * 4 + lane] = 0u;
-      else
-        ((uint16_t *)row)[vecs * 8 + lane] = 0u;
+  while (absent) {
+    const int f = __builtin_ctz(absent), len = __builtin_ctz(~(absent >> f));
+    absent &= ~(((1u << len) - 1u) << f);
+    uint8_t *p = z.table + (r0 + f) * rb, *end = p + len * rb;
+    uint8_t *at = (uint8_t *)((uintptr_t)p & ~(uintptr_t)1023) + (threadIdx.x & 63) * 16;
+    for (; at < end; at += 1024) {
+      if (at >= p && at + 16 <= end) {
+        stream_cols(at, zero);
+      } else {
+#pragma unroll 1
+        for (uint8_t *e = at < p ? p : at; e < at + 16 && e < end; e += z.elem) {
+          if (z.elem == 4)
+            *(uint32_t *)e = 0u;
+          else
+            *(uint16_t *)e = 0u;
+        }
+      }
     }
   }
 }
@@ -131,15 +139,36 @@ __device__ __forceinline__ uint32_t token_key(const void *ids, int is64, int64_t
   return (uint32_t)(id >= 0 && id < rows && id != pad ? id : rows);
 }
 
-// Lanes of the wave with the same digit as this one, among the lanes in `in`.
-__device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, bool in) {
-  uint64_t m = __builtin_amdgcn_ballot_w64(in);
-  for (int b = 0; b < bits; ++b) {
-    const bool one = (d >> b) & 1u;
-    const uint64_t v = __builtin_amdgcn_ballot_w64(one);
-    m &= one ? v : ~v;
+// f(key, position) for the workgroup's positions below n: four loads of a thread are in
+// flight, at position 0 where there is none.
+template <class ID, class F>
+__device__ __forceinline__ void each_key(const ID *__restrict__ ids, int n, int64_t rows,
+                                         int64_t pad, F f) {
+  const int step = blockDim.x;
+  for (int i0 = threadIdx.x; i0 < n; i0 += 4 * step) {
+    int64_t id[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) id[u] = (int64_t)ids[i0 + u * step < n ? i0 + u * step : 0];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i0 + u * step < n)
+        f((uint32_t)(id[u] >= 0 && id[u] < rows && id[u] != pad ? id[u] : rows), i0 + u * step);
   }
-  return m;
+}
+
+// Lanes of the wave with the same digit as this one, among the lanes in `in`.  (Every bit
+// that a digit can have: a loop over those in use took three times the instructions.)
+__device__ __forceinline__ uint64_t same_digit(uint32_t d, bool in) {
+  const uint64_t some = __builtin_amdgcn_ballot_w64(in);
+  uint32_t lo = (uint32_t)some, hi = (uint32_t)(some >> 32);
+#pragma unroll
+  for (int b = 0; b < kDigitBits; ++b) {
+    const uint32_t mine = (uint32_t)((int32_t)(d << (31 - b)) >> 31);   // the bit, 32 times
+    const uint64_t v = __builtin_amdgcn_ballot_w64(mine != 0u);
+    lo &= ~((uint32_t)v ^ mine);
+    hi &= ~((uint32_t)(v >> 32) ^ mine);
+  }
+  return (uint64_t)hi << 32 | lo;
 }
 
 // Exclusive scan of one value per thread over the first kDigits threads of a
@@ -181,10 +210,13 @@ __global__ __launch_bounds__(kSmallWaves * 64) void grad_sort_small(
       const int64_t last = first + slab < z.last ? first + slab : z.last;
       for (int i = tid; i < slab / 32; i += kSmallWaves * 64) occur[i] = 0u;
       __syncthreads();
-      for (int i = tid; i < n; i += kSmallWaves * 64) {
-        const int64_t v = token_key(ids, is64, i, rows, pad);
+      auto mark = [&](uint32_t v, int) {
         if (v >= first && v < last) atomicOr(&occur[(v - first) >> 5], 1u << (v & 31));
-      }
+      };
+      if (is64)
+        each_key((const int64_t *)ids, n, rows, pad, mark);
+      else
+        each_key((const int32_t *)ids, n, rows, pad, mark);
       __syncthreads();
       for (int64_t r = first + wave * 4; r < last; r += kSmallWaves * 4) {
         uint32_t absent = ~(occur[(r - first) >> 5] >> (r & 31)) & 15u;
@@ -195,10 +227,14 @@ __global__ __launch_bounds__(kSmallWaves * 64) void grad_sort_small(
     }
     return;
   }
-  for (int i = tid; i < n; i += kSmallWaves * 64) {
-    key[0][i] = token_key(ids, is64, i, rows, pad);
+  auto enter = [&](uint32_t v, int i) {
+    key[0][i] = v;
     val[0][i] = (uint16_t)i;
-  }
+  };
+  if (is64)
+    each_key((const int64_t *)ids, n, rows, pad, enter);
+  else
+    each_key((const int32_t *)ids, n, rows, pad, enter);
   const int share = ((n + kSmallWaves - 1) / kSmallWaves + 63) & ~63;
   const int lo = wave * share, hi = lo + share < n ? lo + share : n;
   int from = 0;
@@ -230,7 +266,7 @@ __global__ __launch_bounds__(kSmallWaves * 64) void grad_sort_small(
       const bool in = i < hi;
       const uint32_t k = in ? key[from][i] : 0u;
       const uint32_t d = (k >> shift) & mask;
-      const uint64_t same = same_digit(d, bits, in);
+      const uint64_t same = same_digit(d, in);
       if (in) {
         const int rank = __popcll(same & ((1ull << lane) - 1ull));
         const uint32_t at = cnt[wave][d] + rank;
@@ -367,7 +403,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void grad_scatter(
     for (int u = 0; u < kRounds; ++u) {
       const bool in = i0 + u * 64 + lane < whi;
       const uint32_t d = (key[u] >> shift) & mask;
-      const uint64_t same = same_digit(d, bits, in);
+      const uint64_t same = same_digit(d, in);
       if (in) {
         const uint32_t at = cnt[wave][d] + (uint32_t)__popcll(same & ((1ull << lane) - 1ull));
         tok_out[at] = key[u];
@@ -427,6 +463,7 @@ struct Slice {
         RawCols<OT, V> raw;
         float old[V];
         raw.load(row, c);
+        wave_fence();   // (the last lane's neighbour reads some of its columns: before any store)
         raw.decode(old);
 #pragma unroll
         for (int j = 0; j < V; ++j) o[j] += old[j];
@@ -523,8 +560,8 @@ __global__ __launch_bounds__(256) void grad_sums(
       (l ? many : few)[atomicAdd(&count[l], 1u)] = (uint32_t)c;
     }
   } else {
-            S::template write<OT>(table, cur, col, dim, scale, add, acc);
-          }
+    S::template write<OT>(table, cur, col, dim, scale, add, acc);
+  }
 }
 
 // Tokens over several chunks: the sum at the end of the chunk where the token begins
