@@ -37,8 +37,7 @@ struct GradWs {
   uint32_t *count;             // [2]: entries of the lists
   uint32_t *list[2];           // [chunks] each: chunks where a token over several chunks
                                // begins, with few (0) or many (1) of them
-  uint8_t *present;            // [rows, in fours]: 1 for tokens that occur (above kSmallMax
-                               // positions)
+  uint8_t *present;            // [rows, in fours]: 1 for tokens that occur
   float *part;                 // [2 x chunks][dim]: sums of the tokens over a chunk's
                                // start (0) and end (1)
 };
@@ -73,7 +72,7 @@ size_t layout(int64_t n, int64_t rows, int64_t dim, void *base, GradWs *w) {
     at += up256(chunks * 4);
   }
   if (w) w->present = p + at;
-  if (n > kSmallMax) at += up256(rows);
+  at += up256(rows);
   if (w) w->part = (float *)(p + at);
   at += up256(chunks * 2 * dim * 4);
   return (size_t)at;
@@ -191,12 +190,13 @@ __device__ __forceinline__ uint32_t scan_digits(uint32_t v, uint32_t *sums) {
 
 // All passes in one workgroup, keys and positions in LDS; 16 waves, each with a
 // contiguous share and its own digit counters (made exclusive over digits and waves).
-// The workgroups behind the first write the rows of zeros, slabs of `slab` rows each: they
-// find the tokens of a slab themselves.
+// The workgroups behind the first write the rows of zeros below z.last, slabs of `slab` rows
+// each, and note the tokens that occur from there to `stop` for the sums' launch, slabs of
+// `noted` rows each: they find the tokens of their slabs themselves.
 __global__ __launch_bounds__(kSmallWaves * 64) void grad_sort_small(
     const void *__restrict__ ids, int is64, int n, int64_t rows, int64_t pad, int bits, int passes,
     uint32_t *__restrict__ tok, uint32_t *__restrict__ pos, uint32_t *__restrict__ count, Zeros z,
-    int slab) {
+    int64_t stop, int slab, int noted, uint8_t *__restrict__ present) {
   __shared__ uint32_t key[2][kSmallMax];
   __shared__ uint16_t val[2][kSmallMax];
   __shared__ uint32_t cnt[kSmallWaves][kDigits];
@@ -204,20 +204,29 @@ __global__ __launch_bounds__(kSmallWaves * 64) void grad_sort_small(
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (blockIdx.x == 0 && tid < 2) count[tid] = 0u;
   if (blockIdx.x > 0) {
-    uint32_t *occur = key[0];   // a bit per row of the slab (at most 32 kSmallMax)
-    for (int64_t first = (int64_t)(blockIdx.x - 1) * slab; first < z.last;
-         first += (int64_t)(gridDim.x - 1) * slab) {
-      const int64_t last = first + slab < z.last ? first + slab : z.last;
+    uint32_t *occur = key[0], *later = key[1];   // a bit per row (at most 32 kSmallMax each)
+    for (int64_t s = blockIdx.x - 1; s * slab < z.last || z.last + s * noted < stop;
+         s += gridDim.x - 1) {
+      const int64_t first = s * slab, last = first + slab < z.last ? first + slab : z.last;
+      const int64_t from = z.last + s * noted, to = from + noted < stop ? from + noted : stop;
       for (int i = tid; i < slab / 32; i += kSmallWaves * 64) occur[i] = 0u;
+      for (int i = tid; i < noted / 32; i += kSmallWaves * 64) later[i] = 0u;
       __syncthreads();
       auto mark = [&](uint32_t v, int) {
-        if (v >= first && v < last) atomicOr(&occur[(v - first) >> 5], 1u << (v & 31));
+        if (v >= first && v < last)
+          atomicOr(&occur[(v - first) >> 5], 1u << (v & 31));
+        else if (v >= from && v < to)
+          atomicOr(&later[(v - from) >> 5], 1u << (v & 31));
       };
       if (is64)
         each_key((const int64_t *)ids, n, rows, pad, mark);
       else
         each_key((const int32_t *)ids, n, rows, pad, mark);
       __syncthreads();
+      for (int64_t r = from + tid * 4; r < to; r += kSmallWaves * 64 * 4) {
+        const uint32_t here = later[(r - from) >> 5] >> (r & 31) & 15u;
+        *(uint32_t *)(present + r) = here * 0x00204081u & 0x01010101u;   // (a byte per bit)
+      }
       for (int64_t r = first + wave * 4; r < last; r += kSmallWaves * 4) {
         uint32_t absent = ~(occur[(r - first) >> 5] >> (r & 31)) & 15u;
         if (last - r < 4) absent &= (1u << (last - r)) - 1u;
@@ -444,9 +453,17 @@ struct Slice {
   }
 
   __device__ static __forceinline__ void part(float *row, int c, int dim, const float *v) {
+    if (dim >= V) {
+      if (c < dim) {
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (c + j < dim) row[c + j] = v[j];
+        for (int j = 0; j < V; j += 4)
+          store_cols(row + c + j, round_cols<HS_F32, 4>(v + j));
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (c + j < dim) row[c + j] = v[j];
+    }
   }
 
   // table[r] = (add: +=) scale * v
@@ -527,25 +544,27 @@ __global__ __launch_bounds__(256) void grad_sums(
       const int64_t at = (int64_t)(uint32_t)__builtin_amdgcn_readlane(my_pos, i);
       S::load(grad + at * gb, col, dim, v[u]);
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i0 + u < m) {
-        const uint32_t t = __builtin_amdgcn_readlane(my_tok, i0 + u);
-        if (t != cur) {
-          if (head) {
-            S::part(part + (c * 2) * dim, col, dim, acc);
-          } else {
-            S::template write<OT>(table, cur, col, dim, scale, add, acc);
-          }
-#pragma unroll
-          for (int j = 0; j < S::V; ++j) acc[j] = 0.0f;
-          cur = t;
-          head = false;
-          if (cur == none) return;   // (only positions without a token are left)
+    const int end = i0 + U < m ? i0 + U : m;
+#pragma unroll 1
+    for (int i = i0; i < end; ++i) {   // (the next row moves into v[0])
+      const uint32_t t = __builtin_amdgcn_readlane(my_tok, i);
+      if (t != cur) {
+        if (head) {
+          S::part(part + (c * 2) * dim, col, dim, acc);
+        } else {
+          S::template write<OT>(table, cur, col, dim, scale, add, acc);
         }
-        if (cur == none) return;
 #pragma unroll
-        for (int j = 0; j < S::V; ++j) acc[j] += v[u][j];
+        for (int j = 0; j < S::V; ++j) acc[j] = 0.0f;
+        cur = t;
+        head = false;
+      }
+      if (cur == none) return;   // (only positions without a token are left)
+#pragma unroll
+      for (int j = 0; j < S::V; ++j) {
+        acc[j] += v[0][j];
+#pragma unroll
+        for (int u = 0; u + 1 < U; ++u) v[u][j] = v[u + 1][j];
       }
     }
   }
@@ -678,15 +697,26 @@ hipError_t launch_embed_grad(const void *grad, int grad_dtype, const void *ids, 
   Zeros part[3] = {all, all, all};       // of the second count and scatter, of the sums
   int zero_wgs[3] = {0, 0, 0};
   if (n <= kSmallMax) {
-    // slabs: one workgroup for each CU but the sort's; at most as many rows as the bitmap
-    // holds
-    int64_t slab = ((stop + 254) / 255 + 31) / 32 * 32;
-    slab = slab < 32 ? 32 : slab > 32 * kSmallMax ? 32 * kSmallMax : slab;
-    const int64_t wgs = (stop + slab - 1) / slab;
+    // the sort takes about 1.6 us per 1,024 positions, in which the other CUs write some
+    // 10 KiB of zeros for each; the sums' launch, short too, gets the rest
+    const int64_t fit = n * 10240 / (dim * elem) / 32 * 32;
+    Zeros now = all;
+    now.last = n == 0 || fit > stop ? stop : fit;
+    part[2].first = now.last;
+    const int64_t zeros = part[2].last - part[2].first;
+    zero_wgs[2] = (int)((zeros + 15) / 16 < 1024 ? (zeros + 15) / 16 : 1024);
+    // slabs: one workgroup for each CU but the sort's; at most as many rows as the bitmaps
+    // hold
+    auto slab_of = [](int64_t r) {
+      const int64_t slab = ((r + 254) / 255 + 31) / 32 * 32;
+      return slab < 32 ? (int64_t)32 : slab > 32 * kSmallMax ? (int64_t)32 * kSmallMax : slab;
+    };
+    const int64_t slab = slab_of(now.last), noted = slab_of(zeros);
+    int64_t wgs = (now.last + slab - 1) / slab;
+    if (wgs < (zeros + noted - 1) / noted) wgs = (zeros + noted - 1) / noted;
     hipLaunchKernelGGL(grad_sort_small, dim3(1 + (unsigned)(wgs < 255 ? wgs : 255)),
                        dim3(kSmallWaves * 64), 0, st, ids, is64, (int)n, rows, pad, bits, passes,
-                       w.tok[0], w.pos[0], w.count, all, (int)slab);
-    part[2].last = 0;
+                       w.tok[0], w.pos[0], w.count, now, stop, (int)slab, (int)noted, w.present);
   } else {
     int64_t tiles = (n + kTileMin - 1) / kTileMin;
     if (tiles > kTilesMax) tiles = kTilesMax;
