@@ -30,13 +30,13 @@ constexpr int kTilesMax = 64;        // tiles of the sort
 constexpr int kTileMin = 4096;       // positions that make another tile worth it
 constexpr int kChunk = 64;           // sorted places of one wave, at most
 constexpr int kSpanMany = 24;        // chunks that a workgroup instead of a wave joins
+constexpr int kJoinWaves = 8;
 
 struct GradWs {
   uint32_t *tok[2], *pos[2];   // [n] each: sorted keys and positions
   uint32_t *hist;              // [kTilesMax][kDigits]
-  uint32_t *count;             // [2]: entries of the lists
-  uint32_t *list[2];           // [chunks] each: chunks where a token over several chunks
-                               // begins, with few (0) or many (1) of them
+  uint32_t *count;             // [1]: entries of the list
+  uint32_t *many;              // [chunks]: chunks where a token over many chunks begins
   uint8_t *present;            // [rows, in fours]: 1 for tokens that occur
   float *part;                 // [2 x chunks][dim]: sums of the tokens over a chunk's
                                // start (0) and end (1)
@@ -44,11 +44,12 @@ struct GradWs {
 
 __host__ __device__ int64_t up256(int64_t x) { return (x + 255) & ~(int64_t)255; }
 
-// Places per chunk: 64, or fewer while the chunks and column slices (of 512) would
-// not give 2,048 waves (8 per CU).
+// Places per chunk: 64, or fewer while the chunks, their column slices (of 512) and, of rows
+// of up to 256 columns, the chunks that share a wave would not give 2,048 waves (8 per CU).
 int chunk_places(int64_t n, int64_t dim) {
-  int c = kChunk;
-  while (c > 8 && (n + c - 1) / c * ((dim + 511) / 512) < 2048) c >>= 1;
+  int c = kChunk, share = 1;
+  while (share < 64 && dim * share <= 256) share *= 2;
+  while (c > 8 && (n + c - 1) / c * ((dim + 511) / 512) / share < 2048) c >>= 1;
   return c;
 }
 
@@ -67,10 +68,8 @@ size_t layout(int64_t n, int64_t rows, int64_t dim, void *base, GradWs *w) {
   at += (int64_t)kTilesMax * kDigits * 4;
   if (w) w->count = (uint32_t *)(p + at);
   at += 256;
-  for (int i = 0; i < 2; ++i) {
-    if (w) w->list[i] = (uint32_t *)(p + at);
-    at += up256(chunks * 4);
-  }
+  if (w) w->many = (uint32_t *)(p + at);
+  at += up256(chunks * 4);
   if (w) w->present = p + at;
   at += up256(rows);
   if (w) w->part = (float *)(p + at);
@@ -202,7 +201,7 @@ __global__ __launch_bounds__(kSmallWaves * 64) void grad_sort_small(
   __shared__ uint32_t cnt[kSmallWaves][kDigits];
   __shared__ uint32_t sums[kDigits / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (blockIdx.x == 0 && tid < 2) count[tid] = 0u;
+  if (blockIdx.x == 0 && tid == 0) *count = 0u;
   if (blockIdx.x > 0) {
     uint32_t *occur = key[0], *later = key[1];   // a bit per row (at most 32 kSmallMax each)
     for (int64_t s = blockIdx.x - 1; s * slab < z.last || z.last + s * noted < stop;
@@ -310,7 +309,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void grad_count(
     return;
   }
   if (FIRST) {
-    if (blockIdx.x == 0 && threadIdx.x < 2) count[threadIdx.x] = 0u;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *count = 0u;
     for (int64_t i = (int64_t)blockIdx.x * kSortWaves * 64 + threadIdx.x; i < (rows + 3) / 4;
          i += (int64_t)tiles * kSortWaves * 64)
       ((uint32_t *)present)[i] = 0u;
@@ -506,13 +505,21 @@ struct Slice {
   }
 };
 
+// Lists token t, which begins in chunk c, if it goes on for many.  (With every token over
+// two chunks in a list, the atomics took most of the launch: 60 us for 3,000 of them.)
+__device__ __forceinline__ void list_many(const uint32_t *tok, int64_t n, int places, int64_t c,
+                                          uint32_t t, uint32_t *count, uint32_t *many) {
+  const int64_t far = (c + kSpanMany) * places;
+  if (far < n && tok[far] == t) many[atomicAdd(count, 1u)] = (uint32_t)c;
+}
+
 template <int DT, int OT>
 __global__ __launch_bounds__(256) void grad_sums(
     const uint8_t *__restrict__ grad, const uint32_t *__restrict__ tok,
     const uint32_t *__restrict__ pos, int64_t n, int64_t rows, int dim, int places,
     int64_t chunks, int slices, int64_t sum_blocks, float scale, int add,
-    float *__restrict__ part, uint32_t *__restrict__ count, uint32_t *__restrict__ few,
-    uint32_t *__restrict__ many, uint8_t *__restrict__ table,
+    float *__restrict__ part, uint32_t *__restrict__ count, uint32_t *__restrict__ many,
+    uint8_t *__restrict__ table,
     const uint8_t *__restrict__ present, Zeros z) {
   using S = Slice<DT>;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -573,11 +580,81 @@ __global__ __launch_bounds__(256) void grad_sums(
     S::part(part + (c * 2) * dim, col, dim, acc);
   } else if (cur == next) {
     S::part(part + (c * 2 + 1) * dim, col, dim, acc);
-    if (slice == 0 && lane == 0) {
-      const int64_t far = (c + kSpanMany) * places;
-      const int l = far < n && tok[far] == cur ? 1 : 0;
-      (l ? many : few)[atomicAdd(&count[l], 1u)] = (uint32_t)c;
+    if (slice == 0 && lane == 0) list_many(tok, n, places, c, cur, count, many);
+  } else {
+    S::template write<OT>(table, cur, col, dim, scale, add, acc);
+  }
+}
+
+// The same for rows that half a wave or less takes: `lanes` lanes (a power of two) have a
+// chunk each.  (200,000 bf16 rows of 64 columns with a wave for each chunk: 65 us.)
+template <int DT, int OT>
+__global__ __launch_bounds__(256) void grad_sums_narrow(
+    const uint8_t *__restrict__ grad, const uint32_t *__restrict__ tok,
+    const uint32_t *__restrict__ pos, int64_t n, int64_t rows, int dim, int places,
+    int64_t chunks, int lanes, int64_t sum_blocks, float scale, int add,
+    float *__restrict__ part, uint32_t *__restrict__ count, uint32_t *__restrict__ many,
+    uint8_t *__restrict__ table,
+    const uint8_t *__restrict__ present, Zeros z) {
+  using S = Slice<DT>;
+  if ((int64_t)blockIdx.x >= sum_blocks) {
+    zero_rows(z, present, (int64_t)blockIdx.x - sum_blocks, (int64_t)gridDim.x - sum_blocks);
+    return;
+  }
+  const int lane = threadIdx.x & (lanes - 1), col = S::column(0, lane, dim);
+  const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
+  if (c >= chunks) return;
+  const int64_t lo = c * places;
+  const int m = (int)(n - lo < places ? n - lo : places);
+  const uint32_t none = (uint32_t)rows;
+  const uint32_t prev = lo > 0 ? tok[lo - 1] : none;
+  const uint32_t next = lo + m < n ? tok[lo + m] : none;
+  const int64_t gb = row_bytes<DT>(dim);
+  float acc[S::V] = {};
+  uint32_t cur = tok[lo];
+  bool head = cur == prev;
+  constexpr int U = 8;
+  for (int i0 = 0; i0 < m; i0 += U) {
+    uint32_t t[U], p[U];
+    float v[U][S::V];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = lo + (i0 + u < m ? i0 + u : m - 1);
+      t[u] = tok[i];
+      p[u] = pos[i];
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u) S::load(grad + (int64_t)p[u] * gb, col, dim, v[u]);
+    const int end = i0 + U < m ? i0 + U : m;
+#pragma unroll 1
+    for (int i = i0; i < end; ++i) {   // (the next row moves into v[0])
+      if (t[0] != cur) {
+        if (head) {
+          S::part(part + (c * 2) * dim, col, dim, acc);
+        } else {
+          S::template write<OT>(table, cur, col, dim, scale, add, acc);
+        }
+#pragma unroll
+        for (int j = 0; j < S::V; ++j) acc[j] = 0.0f;
+        cur = t[0];
+        head = false;
+      }
+      if (cur == none) return;
+#pragma unroll
+      for (int u = 0; u + 1 < U; ++u) t[u] = t[u + 1];
+#pragma unroll
+      for (int j = 0; j < S::V; ++j) {
+        acc[j] += v[0][j];
+#pragma unroll
+        for (int u = 0; u + 1 < U; ++u) v[u][j] = v[u + 1][j];
+      }
+    }
+  }
+  if (head) {
+    S::part(part + (c * 2) * dim, col, dim, acc);
+  } else if (cur == next) {
+    S::part(part + (c * 2 + 1) * dim, col, dim, acc);
+    if (lane == 0) list_many(tok, n, places, c, cur, count, many);
   } else {
     S::template write<OT>(table, cur, col, dim, scale, add, acc);
   }
@@ -585,8 +662,8 @@ __global__ __launch_bounds__(256) void grad_sums(
 
 // Tokens over several chunks: the sum at the end of the chunk where the token begins
 // and those at the start of the following ones.  A wave joins a few chunks, 256 columns at
-// a time, in order; a workgroup many, 64 columns at a time, in four contiguous shares
-// whose sums are added in order.
+// a time, in order; a workgroup many, 64 columns at a time, in a contiguous share for each
+// of its waves, whose sums are added in order.
 template <int OT>
 __device__ __forceinline__ void join_write(uint8_t *table, int64_t t, int c, int dim, float x,
                                            int add) {
@@ -595,15 +672,15 @@ __device__ __forceinline__ void join_write(uint8_t *table, int64_t t, int c, int
 }
 
 template <int OT>
-__global__ __launch_bounds__(256) void grad_join(
-    const uint32_t *__restrict__ tok, int64_t n, int dim, int places, int64_t chunks,
-    float scale, int add, const uint32_t *__restrict__ count, const uint32_t *__restrict__ few,
+__global__ __launch_bounds__(kJoinWaves * 64) void grad_join(
+    const uint32_t *__restrict__ tok, int64_t n, int64_t rows, int dim, int places,
+    int64_t chunks, float scale, int add, const uint32_t *__restrict__ count,
     const uint32_t *__restrict__ many, const float *__restrict__ part,
     uint8_t *__restrict__ table) {
-  __shared__ float sums[4][64];
+  __shared__ float sums[kJoinWaves][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int many_blocks = (dim + 63) / 64, few_blocks = (dim + 255) / 256;
-  const int64_t n_many = (int64_t)count[1] * many_blocks, n_few = (int64_t)count[0] * few_blocks;
+  const int64_t n_many = (int64_t)*count * many_blocks, n_few = (chunks - 1) * few_blocks;
   for (int64_t task = blockIdx.x; task < n_many; task += gridDim.x) {
     const int64_t e = task / many_blocks, c = many[e];
     const int col = (int)(task - e * many_blocks) * 64 + lane, cc = col < dim ? col : 0;
@@ -615,7 +692,7 @@ __global__ __launch_bounds__(256) void grad_join(
       lo += step * __popcll(__builtin_amdgcn_ballot_w64(k < hi && tok[k * places] == t));
       hi = hi < lo + step ? hi : lo + step;
     }
-    const int64_t c1 = lo, share = (c1 - c + 3) / 4;
+    const int64_t c1 = lo, share = (c1 - c + kJoinWaves - 1) / kJoinWaves;
     const int64_t a = c + 1 + wave * share, b = a + share < c1 + 1 ? a + share : c1 + 1;
     float v = wave == 0 ? part[(c * 2 + 1) * dim + cc] : 0.0f;
     // (16 in flight: with four, a token in 15,000 of 262,144 places took most of the launch)
@@ -624,18 +701,27 @@ __global__ __launch_bounds__(256) void grad_join(
     sums[wave][lane] = v;
     __syncthreads();
     if (wave == 0) {
-      v = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
+#pragma unroll
+      for (int w = 1; w < kJoinWaves; ++w) v += sums[w][lane];
       join_write<OT>(table, t, col, dim, v * scale, add);
     }
     __syncthreads();
   }
-  for (int64_t task = (int64_t)blockIdx.x * 4 + wave; task < n_few; task += (int64_t)gridDim.x * 4) {
-    const int64_t e = task / few_blocks, c = few[e];
-    const int col = (int)(task - e * few_blocks) * 256 + lane;
+  for (int64_t task = (int64_t)blockIdx.x * kJoinWaves + wave; task < n_few;
+       task += (int64_t)gridDim.x * kJoinWaves) {
+    const int64_t c = task / few_blocks;
+    const int col = (int)(task - c * few_blocks) * 256 + lane;
     const uint32_t t = tok[(c + 1) * places - 1];
-    const int64_t k0 = c + 1 + lane;   // chunks that begin with it: below kSpanMany of them
-    const int64_t c1 = c + __popcll(__builtin_amdgcn_ballot_w64(
-                               lane < kSpanMany && k0 < chunks && tok[k0 * places] == t));
+    // whether it goes on in the next chunk, and began in this one
+    const uint32_t first = tok[c * places], before = c > 0 ? tok[c * places - 1] : (uint32_t)rows;
+    const int64_t k0 = c + 1 + lane < chunks ? c + 1 + lane : chunks - 1;
+    const uint64_t same = __builtin_amdgcn_ballot_w64(tok[k0 * places] == t);
+    if (t == (uint32_t)rows || !(same & 1u) || (first == t && before == t)) continue;
+    // chunks that begin with it (past the last chunk, the last one is looked at again)
+    const int more = ~same ? __builtin_ctzll(~same) : 64;
+    const int left = (int)(chunks - 1 - c < 64 ? chunks - 1 - c : 64);
+    const int64_t c1 = c + (more < left ? more : left);
+    if (c1 - c >= kSpanMany) continue;   // (in the list)
     float v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -658,18 +744,21 @@ hipError_t launch_sums(const GradWs &w, int side, const void *grad, int64_t n, i
   const int places = chunk_places(n, dim);
   const int64_t chunks = (n + places - 1) / places;
   const int slices = (int)((dim + 64 * V - 1) / (64 * V));
-  const int64_t sum_blocks = (chunks * slices + 3) / 4;
-  hipLaunchKernelGGL((grad_sums<DT, OT>),
+  int lanes = 1;   // that a row takes
+  while (lanes < 64 && lanes * V < dim) lanes *= 2;
+  const bool narrow = lanes < 64;
+  const int64_t sum_blocks = narrow ? (chunks * lanes + 255) / 256 : (chunks * slices + 3) / 4;
+  hipLaunchKernelGGL((narrow ? grad_sums_narrow<DT, OT> : grad_sums<DT, OT>),
                      dim3((unsigned)(sum_blocks + zero_wgs)), dim3(256), 0, st,
                      (const uint8_t *)grad, w.tok[side], w.pos[side], n, rows, (int)dim, places,
-                     chunks, slices, sum_blocks, scale, add, w.part, w.count, w.list[0],
-                     w.list[1], (uint8_t *)table, w.present, z);
+                     chunks, narrow ? lanes : slices, sum_blocks, scale, add, w.part, w.count,
+                     w.many, (uint8_t *)table, w.present, z);
   if (chunks > 1) {
     // (as many tasks at most, in waves)
-    const int64_t tasks = ((chunks - 1) * ((dim + 255) / 256) + 3) / 4;
-    hipLaunchKernelGGL(grad_join<OT>, dim3((unsigned)(tasks < 1024 ? tasks : 1024)), dim3(256), 0,
-                       st, w.tok[side], n, (int)dim, places, chunks, scale, add, w.count,
-                       w.list[0], w.list[1], w.part, (uint8_t *)table);
+    const int64_t tasks = ((chunks - 1) * ((dim + 255) / 256) + kJoinWaves - 1) / kJoinWaves;
+    hipLaunchKernelGGL(grad_join<OT>, dim3((unsigned)(tasks < 512 ? tasks : 512)),
+                       dim3(kJoinWaves * 64), 0, st, w.tok[side], n, rows, (int)dim, places, chunks, scale, add, w.count,
+                       w.many, w.part, (uint8_t *)table);
   }
   return hipGetLastError();
 }
