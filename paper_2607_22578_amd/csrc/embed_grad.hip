@@ -27,7 +27,7 @@ constexpr int kDigitBits = 9;        // most bits of a digit
 constexpr int kDigits = 1 << kDigitBits;
 static_assert(kSortWaves * 64 == 2 * kDigits, "two threads per digit");
 constexpr int kTilesMax = 64;        // tiles of the sort
-constexpr int kTileMin = 4096;       // positions that make another tile worth it
+constexpr int kTileMin = 1024;       // positions that make another tile worth it
 constexpr int kChunk = 64;           // sorted places of one wave, at most
 constexpr int kSpanMany = 24;        // chunks that a workgroup instead of a wave joins
 constexpr int kJoinWaves = 8;
