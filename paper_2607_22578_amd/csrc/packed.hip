@@ -234,7 +234,7 @@ template <int XT>
 __device__ __forceinline__ void stage_x(const uint8_t *x, int64_t m0, int m, int dim, int c0,
                                         int cols, int row_bytes, int part_bytes, uint8_t *lds) {
   const int vecs = cols / 8;
-  for (int i = threadIdx.x; i < m * vecs; i += 256) {
+  for (int i = threadIdx.x; i < m * vecs; i += blockDim.x) {
     const int r = i / vecs, c = (i - r * vecs) * 8;
     uint8_t *to = lds + r * row_bytes + c * 2;
     const bool in = c0 + c < dim;
@@ -269,22 +269,26 @@ __device__ __forceinline__ void stage_x(const uint8_t *x, int64_t m0, int m, int
   }
 }
 
-// Workgroups of four waves that loop over items: ks of the waves share the columns
-// (block kb goes to wave kb % ks; their sums are joined in LDS, in wave order), 4 / ks
-// have 16 NT table rows each.  MT tiles of 16 rows of x, staged `chunk` columns at a
+// Workgroups of four or kWaves<MT> waves that loop over items: ks of the waves share the
+// columns (block kb goes to wave kb % ks; their sums are joined in LDS, in wave order), each
+// ks of them have 16 NT table rows.  MT tiles of 16 rows of x, staged `chunk` columns at a
 // time, once if that is all of them.  The next block's loads, also those of the next
 // item's first, are in flight while a block is multiplied.
+template <int MT>
+constexpr int kWaves = MT == 1 ? 16 : 8;
+
 template <int XT, int GROUP, int MT, int NT, int MODE>
-__global__ __launch_bounds__(256, MT == 1 ? 4 : 2) void score_packed_kernel(
+__global__ __launch_bounds__(kWaves<MT> * 64, MT == 1 ? 4 : 2) void score_packed_kernel(
     const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales, int scale_bf16,
     int64_t rows, int dim,
     const uint8_t *__restrict__ x, int64_t n_x, int ks, int chunk, int64_t row_blocks,
     int64_t items, void *__restrict__ out, int out_f32, int64_t out_stride) {
   constexpr int PARTS = XT == HS_F32 ? 3 : 1;
   extern __shared__ __align__(16) uint8_t lds[];
-  f32x4_t *joined = (f32x4_t *)lds;   // [3][NT * MT][64] where ks > 1
-  uint8_t *xs = lds + (ks > 1 ? 3 * NT * MT * 64 * 16 : 0);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int sets = (int)(blockDim.x >> 6) / ks;   // of 16 NT table rows
+  f32x4_t *joined = (f32x4_t *)lds;   // [sets * (ks - 1)][NT * MT][64]
+  uint8_t *xs = lds + sets * (ks - 1) * NT * MT * 64 * 16;
   const int i16 = lane & 15, p = lane >> 4;
   const int part_of = wave % ks;
   const int blocks = (dim + kBlock - 1) / kBlock;
@@ -298,7 +302,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 4 : 2) void score_packed_kernel(
   int l_step = 0;
   auto point = [&]() {
     const int64_t rb = l_item % row_blocks;
-    const int64_t n0 = (rb * (4 / ks) + wave / ks) * (16 * NT);
+    const int64_t n0 = (rb * sets + wave / ks) * (16 * NT);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       // (rows past the last are stood in for by the last: their sums are not stored)
@@ -363,7 +367,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 4 : 2) void score_packed_kernel(
     if (++step < steps) return;
     step = 0;
     item += gridDim.x;
-    // (ks = 4: waves 1-3 into wave 0; ks = 2: waves 1 and 3 into 0 and 2)
+    // (into the first of the ks waves)
     if (ks > 1) {
       __syncthreads();   // (the last item's sums are read)
       if (part_of > 0) {
@@ -371,7 +375,7 @@ __global__ __launch_bounds__(256, MT == 1 ? 4 : 2) void score_packed_kernel(
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int m = 0; m < MT; ++m)
-            joined[((wave - 1) * NT * MT + t * MT + m) * 64 + lane] = tot[t][m];
+            joined[((wave - wave / ks - 1) * NT * MT + t * MT + m) * 64 + lane] = tot[t][m];
       }
       __syncthreads();
       if (part_of > 0) return;
@@ -380,14 +384,15 @@ __global__ __launch_bounds__(256, MT == 1 ? 4 : 2) void score_packed_kernel(
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int m = 0; m < MT; ++m) {
-            const f32x4_t o = joined[((wave + q - 1) * NT * MT + t * MT + m) * 64 + lane];
+            const f32x4_t o =
+                joined[((wave - wave / ks + q - 1) * NT * MT + t * MT + m) * 64 + lane];
 #pragma unroll
             for (int i = 0; i < 4; ++i) tot[t][m][i] += o[i];
           }
       }
     }
     // lane l holds table row l % 16 of a tile and rows 4 (l / 16) .. + 3 of x
-    const int64_t n0 = (rb * (4 / ks) + wave / ks) * (16 * NT);
+    const int64_t n0 = (rb * sets + wave / ks) * (16 * NT);
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -426,33 +431,59 @@ hipError_t launch_packed_t(const hs_row_table *t, const void *x, int64_t n_x, vo
   // the columns shared by up to four waves while there are fewer than 4,096 (16 per CU)
   int ks = 1;
   while (ks < 4 && waves * ks < 4096 && t->dim > kBlock * ks) ks *= 2;
-  // x is staged whole where that leaves room for more workgroups on a CU or at least one
-  // of them; else by as many of the ks waves' steps as fit, at least one
+  // x is staged whole where that leaves room for more workgroups of four waves on a CU;
+  // else one workgroup has as many waves, and stages it whole or a part at a time (with four
+  // waves 5 fp32 rows x 66,088 x 3,712 took 90 us, 48 with 16)
   const int mrows = (int)(n_x < 16 * MT ? n_x : 16 * MT), parts = XT == HS_F32 ? 3 : 1;
-  const int nb = (int)((t->dim + kBlock - 1) / kBlock);
+  const int nb = (int)((t->dim + kBlock - 1) / kBlock), cus = persistent_grid();
+  int wgs = MT == 1 ? 3 : 2, n_waves = 4;
+  auto whole = [&](int k) { return (nb + k - 1) / k * k; };
   auto staged = [&](int blocks) { return (size_t)mrows * parts * (blocks * kBlock * 2 + 16); };
-  const size_t joined = (size_t)3 * NT * MT * 64 * 16;
-  int wgs = MT == 1 ? 3 : 2, chunk = (nb + ks - 1) / ks * ks;
+  auto joined = [&](int k) { return (size_t)(n_waves - n_waves / k) * NT * MT * 64 * 16; };
+  int chunk = whole(ks);
   if (staged(chunk) > kStageMax) {
-    if (staged(chunk) + joined <= kLds) {
-      wgs = 1;
+    wgs = 1;
+    n_waves = kWaves<MT>;
+    auto items = [&](int k) { return (waves + n_waves / k - 1) / (n_waves / k); };
+    // (not whole, either, where the sums to be joined take the room that would let more CUs
+    // have an item: see below)
+    const bool few = nb > 1 && items(1) * 2 <= cus && staged(whole(2)) + joined(2) > kLds;
+    if (staged(whole(1)) <= kLds && !few) {
+      // the fewest steps one after another (ks = 4 against 1: 5 fp32 rows x 66,088 x 3,712 48
+      // against 61 us, 30 bf16 rows x 150,000 x 1,280 52 against 31), and a join's time
+      int64_t best = INT64_MAX;
+      for (int k = 1; k <= 4 && staged(whole(k)) + joined(k) <= kLds; k *= 2) {
+        const int64_t steps = 4 * (whole(k) / k) + (k > 1 ? 1 + NT * MT : 1);   // in quarters
+        const int64_t cost = (items(k) + cus - 1) / cus * steps;
+        if (cost < best) {
+          best = cost;
+          ks = k;
+        }
+      }
+      chunk = whole(ks);
     } else {
-      const int fit = (kStageMax / (mrows * parts) - 16) / (2 * kBlock);   // blocks
-      while (ks > fit) ks /= 2;
-      chunk = fit / ks * ks;
+      // every item stages x anew, so as many table rows share that as leave each CU one (48
+      // bf16 rows x 100,000 x 4,096 147 -> 95 us; 35 x 15,726 x 2,048 26 us with ks = 1, 19
+      // with 4)
+      auto fit = [&](int k) {
+        return (int)((kLds - joined(k)) / (mrows * parts) - 16) / (2 * kBlock);
+      };
+      for (ks = 1; ks < 4 && items(ks) * 2 <= cus && fit(2 * ks) >= 2 * ks;) ks *= 2;
+      chunk = fit(ks) / ks * ks;
     }
   }
-  const int64_t per = 16 * NT * (4 / ks), row_blocks = (t->rows + per - 1) / per;
+  const int64_t per = 16 * NT * (n_waves / ks), row_blocks = (t->rows + per - 1) / per;
   const int64_t items = row_blocks * mblocks;
-  const size_t lds = staged(chunk) + (ks > 1 ? joined : 0);
+  const size_t lds = staged(chunk) + joined(ks);
   const bool bf16 = t->scale_dtype == HS_BF16;
   auto kernel = !bf16 || t->dim < kBlock ? score_packed_kernel<XT, GROUP, MT, NT, kEach>
                 : t->dim % kBlock        ? score_packed_kernel<XT, GROUP, MT, NT, kTail>
                                          : score_packed_kernel<XT, GROUP, MT, NT, kWhole>;
   // (workgroups per CU: 24 rows x 1M x 768 took 105 us with two, 114 with four; one row
   // x 32,000 x 4,096 18 us with three or four, 20 with two)
-  const int64_t grid = wgs * (int64_t)persistent_grid();
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(items < grid ? items : grid)), dim3(256), lds, st,
+  const int64_t grid = wgs * (int64_t)cus;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(items < grid ? items : grid)),
+                     dim3(n_waves * 64), lds, st,
                      (const uint8_t *)t->data, (const uint8_t *)t->scale, (int)bf16, t->rows,
                      (int)t->dim, (const uint8_t *)x, n_x, ks, chunk * kBlock, row_blocks, items,
                      out, (int)(out_dtype == HS_F32), out_stride);
