@@ -39,6 +39,32 @@ def test_score_packed_sizes(group, dim, xt):
         ref.check(got, want, bound, out, f"m={m} rows={rows} dim={dim} group={group}")
 
 
+@pytest.mark.parametrize("m,rows,dim,group,xt,sdt", [
+    # x staged whole by 16 or 8 waves: four, two and one of them share the columns
+    (5, 66_001, 3712, 64, F32, BF16), (12, 1000, 3200, 32, BF16, F32), (13, 9001, 3328, 128, BF16, BF16),
+    (30, 33_333, 1280, 64, BF16, BF16), (7, 9001, 1472, 32, F32, BF16), (40, 20_001, 1056, 32, BF16, F32), (16, 70_001, 2048, 64, BF16, BF16),
+    # in parts: for many rows, few, rows of x in several blocks, the widest
+    (16, 40_001, 2080, 32, F32, BF16), (22, 30_001, 1184, 32, F32, F32), (35, 1573, 2048, 128, BF16, F32),
+    (48, 40_001, 2176, 128, BF16, BF16), (16, 300, 4096, 32, F32, BF16), (70, 600, 2304, 64, BF16, BF16),
+    (37, 1001, 2304, 32, F32, BF16), (3, 97, 16_384, 128, F32, BF16), (64, 97, 16_384, 64, BF16, F32)])
+def test_score_packed_staging(m, rows, dim, group, xt, sdt):
+    g = torch.Generator().manual_seed(m + rows)
+    codes = torch.randint(0, 256, (rows, dim // 2), dtype=torch.uint8, generator=g)
+    scales = (torch.randn(rows, dim // group, generator=g) * 0.1).to(sdt)
+    table = hs.RowTable(codes.to(device()), scales.to(device()), group=group)
+    x = torch.randn(m, dim, generator=g).to(xt)
+    got = hs.score_packed(table, x.to(device()))
+    # (a part of the rows: the ends and some between)
+    some = torch.unique(torch.cat([torch.arange(min(rows, 300)),
+                                   torch.randint(0, rows, (300,), generator=g),
+                                   torch.arange(max(rows - 300, 0), rows)]))
+    values = ref.unpack(codes[some], scales[some], group)
+    want, bound = ref.score_packed(values, ref.f64(x), group)
+    ref.check(got[:, some.to(device())], want, bound, F32)
+    assert torch.isfinite(got).all()
+    assert torch.equal(got, hs.score_packed(table, x.to(device())))
+
+
 def test_score_packed_places_every_column():
     """One-hot rows pick single table columns: exact, so any mixed-up column shows."""
     rng = np.random.default_rng(3)
