@@ -8,7 +8,7 @@
 // replaced from the table.  A range with more marked columns than the table holds is
 // taken in halves.
 // Bound by the scores' bytes.  256 x 131,072 bf16, 1,000 tokens seen and 25 biases on
-// average, a mask per row (140 MB): 38 us, 3.7 TB/s (35 without lists).  (Counts in two words per column of a
+// average, a mask per row (140 MB): 39 us, 3.6 TB/s (35 without lists).  (Counts in two words per column of a
 // 4,096-column tile took 53 to 70 us, with the chain of list, marks and scores paid
 // for each tile.)
 #include "rows.h"

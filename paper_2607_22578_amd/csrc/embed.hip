@@ -9,7 +9,7 @@ namespace hs {
 //
 // A group of threads makes one row; a thread makes 16 bytes of it at a time, so a wave
 // stores whole row segments, as the byte gather does (hs_scatter).  Bound by the bytes:
-// 65,536 tokens from a 131,072 x 4,096 table in four bits (583 MB): 87 us, 6.7 TB/s.
+// 65,536 tokens from a 131,072 x 4,096 table in four bits (583 MB): 90 us, 6.5 TB/s.
 template <int DT, int OT>
 __global__ __launch_bounds__(256) void embed_kernel(
     const uint8_t *__restrict__ data, const void *__restrict__ scales, int scale_bf16,

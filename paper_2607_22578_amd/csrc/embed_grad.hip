@@ -5,14 +5,18 @@
 //           in ascending order; positions that stand for no token take the key
 //           `rows`, behind all others.  Up to kSmallMax positions in one workgroup;
 //           above, two launches per digit (counts per tile, scatter).
-//   sums    the sorted places in chunks of at most 64: a wave adds up the rows of
-//           its chunk for one slice of columns, place after place, in registers, and
+//   sums    the sorted places in chunks of at most 64: a wave (or, of narrow rows, a few
+//           lanes) adds up the rows of its chunk for one slice of columns, place after place, in registers, and
 //           writes a row whenever the token changes.  The work per wave does not depend
 //           on how often tokens occur.  Tokens that reach over a chunk's end leave
 //           partial sums.
 //   join    partial sums of the tokens over several chunks, in chunk order.
 // Every row's additions are thus in an order that the sizes and ids fix.
-// Floor: dO once, dT once; the keys are small beside them.
+// Floor: dO once, dT once; the keys are small beside them.  262,144 bf16 rows of 1,024
+// columns for 131,072 tokens, fp32 gradient (1,075 MB): 268 us; the sums' launch (877 MB of
+// it) 192 us, 4.6 TB/s, a copy's rate; the sort 40 us beside zeros.  10,007 fp32 rows of 771
+// for 50,257 (186 MB): 50 us; 2,048 bf16 rows of 1,024 for 32,000 (70 MB): 25 us, of which
+// 20 are the latency of three launches, whatever zeros are written beside them.
 #include "rows.h"
 
 namespace hs {
@@ -79,8 +83,8 @@ size_t layout(int64_t n, int64_t rows, int64_t dim, void *base, GradWs *w) {
 
 // ---------------------------------------------------------------- rows of zeros
 //
-// The sort's launches leave most CUs idle, so further workgroups of theirs write the rows
-// of tokens that do not occur.
+// The sort's launches leave most CUs idle, so further workgroups of theirs, and some of the
+// sums', write the rows of tokens that do not occur.
 struct Zeros {
   uint8_t *table;
   int64_t first, last;    // rows that are looked at, from a multiple of 4 on
