@@ -137,6 +137,33 @@ def test_embed_grad_sizes(n, rows, dim, din, dout):
     run_grad(rng, n, rows, dim, din, dout, torch.int64 if n % 2 else torch.int32)
 
 
+@pytest.mark.parametrize("n,rows,dim", [(1, 9001, 515), (40, 30_001, 515), (7, 70_000, 33),
+                                        (300, 20_003, 2049), (2000, 40_000, 1)])
+@pytest.mark.parametrize("din,dout", [(F32, BF16), (BF16, F32)])
+def test_embed_grad_few_tokens_of_many(n, rows, dim, din, dout):
+    """Rows of zeros of odd widths, written by both launches."""
+    rng = np.random.default_rng(n + rows)
+    ids = rng.integers(0, rows, n)
+    ids[:2] = (rows - 1, 0)[:n]
+    run_grad(rng, n, rows, dim, din, dout, ids=ids)
+
+
+@pytest.mark.parametrize("dim,din", [(3, F32), (20, BF16), (128, F32), (129, F32), (256, BF16),
+                                     (264, BF16)])
+def test_embed_grad_runs_over_chunk_ends(dim, din):
+    """Tokens of lengths around multiples of 8 to 64 places, and over 23 to 70 of those."""
+    rng = np.random.default_rng(dim)
+    runs = [8, 1, 7, 16, 9, 63, 64, 65, 128] + [c * k + e for c in (8, 16, 64)
+                                              for k in (22, 23, 24, 25) for e in (-1, 0, 1)]
+    runs += [8 * 63, 8 * 64, 8 * 65 + 1, 16 * 70, 64 * 70, 1, 64 * 30 + 5]
+    for lengths in (runs, runs[::-1], [64 * 24], [8 * 24, 8 * 24], [5000, 1, 9000]):
+        ids = np.repeat(np.arange(len(lengths)), lengths)
+        run_grad(rng, len(ids), len(lengths), dim, din, F32, ids=rng.permutation(ids))
+    # and where chunks have 64 places
+    ids = np.concatenate([np.repeat(np.arange(len(runs)), runs), np.arange(len(runs), 200_000)])
+    run_grad(rng, len(ids), 200_000, dim, din, F32, ids=rng.permutation(ids))
+
+
 @pytest.mark.parametrize("dim", [64, 101, 1544])
 @pytest.mark.parametrize("dout", [F32, BF16])
 def test_embed_grad_accumulate_and_padding(dim, dout):
