@@ -30,7 +30,9 @@ namespace {
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kBlock = 256;            // columns per step of a wave
-constexpr int kStageMax = 56 * 1024;     // LDS bytes of staged x, for two workgroups a CU
+// LDS bytes of staged x that leave room for three (MT = 1) or two workgroups a CU
+template <int MT>
+constexpr int kStageMax = (MT == 1 ? 48 : 56) * 1024;
 constexpr int kLds = 158 * 1024;         // of a CU, for one
 
 __device__ __forceinline__ bf16x8_t decode_codes(uint32_t w) {
@@ -442,7 +444,7 @@ hipError_t launch_packed_t(const hs_row_table *t, const void *x, int64_t n_x, vo
   auto staged = [&](int blocks) { return (size_t)mrows * parts * (blocks * kBlock * 2 + 16); };
   auto joined = [&](int k) { return (size_t)(n_waves - n_waves / k) * NT * MT * 64 * 16; };
   int chunk = whole(ks);
-  if (staged(chunk) > kStageMax) {
+  if (staged(chunk) > kStageMax<MT>) {
     wgs = 1;
     n_waves = kWaves<MT>;
     auto items = [&](int k) { return (waves + n_waves / k - 1) / (n_waves / k); };
