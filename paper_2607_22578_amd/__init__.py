@@ -820,23 +820,25 @@ def _tensor(t, what: str, device, shape=None, dtypes=None):
 
 def _arg(t, what: str, device, shape, dtype):
     """Address of one checked contiguous device tensor."""
-    if t.dtype is dtype and t.device == device and (shape is None or t.shape == shape) and \
-            t.is_contiguous():
+    if t.dtype is dtype and t.get_device() == device.index and \
+            (shape is None or t.shape == shape) and t.is_contiguous():
         return t.data_ptr()
     return _tensor(t, what, device, shape, (dtype,)).data_ptr()
 
 
 def _rows_of(t, what: str):
-    """Row stride of a 2-D tensor whose rows are contiguous."""
+    """(rows, columns, row stride) of a 2-D tensor whose rows are contiguous."""
     if t.dim() != 2:
         raise ValueError(f"{what} must be 2-D")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    rows, cols = t.shape
+    stride, step = t.stride()
+    if cols > 1 and step != 1:
         raise ValueError(f"{what} must have contiguous rows")
-    if t.shape[0] > 1:
-        if t.stride(0) < t.shape[1]:
+    if rows > 1:
+        if stride < cols:
             raise ValueError(f"{what} has overlapping rows")
-        return t.stride(0)
-    return t.shape[1]
+        return rows, cols, stride
+    return rows, cols, cols
 
 
 class RowTable:
@@ -969,7 +971,7 @@ def score_packed(table: RowTable, x, out_dtype=None, out=None, stream=None):
     with ctx:
         if out is None:
             out = torch.empty((m, table.rows), dtype=out_dtype or torch.float32, device=device)
-        stride = _rows_of(out, "out")
+        stride = _rows_of(out, "out")[2]
         if out.device != device or out.shape != (m, table.rows) or \
                 out_dtype not in (None, out.dtype):
             raise ValueError("out does not fit the table, x and out_dtype")
@@ -989,9 +991,8 @@ def adjust_scores(scores, allow=None, seen=None, seen_off=None, prompt_len=None,
     [rows x words].  `out` may be scores; by default a new tensor."""
     torch = _torch
     device = scores.device
-    stride = _rows_of(scores, "scores")
+    rows, cols, stride = _rows_of(scores, "scores")
     code = _float_code(scores.dtype, "scores")
-    rows, cols = scores.shape
     if (seen is None) != (seen_off is None):
         raise ValueError("seen and seen_off belong together")
     if not (bias_id is None) == (bias is None) == (bias_off is None):
@@ -1027,10 +1028,12 @@ def adjust_scores(scores, allow=None, seen=None, seen_off=None, prompt_len=None,
     with ctx:
         if out is None:
             out = torch.empty((rows, cols), dtype=scores.dtype, device=device)
-        elif out.device != device or out.shape != scores.shape or out.dtype != scores.dtype:
-            raise ValueError("out does not fit scores")
-        hs_adjust_scores(a, scores, stride, out, _rows_of(out, "out"), code, rows, cols,
-                         stream=stream)
+            out_stride = cols
+        else:
+            *shape, out_stride = _rows_of(out, "out")
+            if out.device != device or shape != [rows, cols] or out.dtype != scores.dtype:
+                raise ValueError("out does not fit scores")
+        hs_adjust_scores(a, scores, stride, out, out_stride, code, rows, cols, stream=stream)
     return out
 
 
@@ -1042,9 +1045,8 @@ def topk_rows(scores, k: int, out=None, ws=None, stream=None):
     hs_topk_rows_bytes' size."""
     torch = _torch
     device = scores.device
-    stride = _rows_of(scores, "scores")
+    rows, cols, stride = _rows_of(scores, "scores")
     code = _float_code(scores.dtype, "scores")
-    rows, cols = scores.shape
     need = hs_topk_rows_bytes(rows, cols, k) if ws is None else 0
     ctx, stream = _on(stream, device)
     with ctx:
@@ -1053,8 +1055,8 @@ def topk_rows(scores, k: int, out=None, ws=None, stream=None):
                    torch.empty((rows, k), dtype=torch.int32, device=device))
         if ws is None:
             ws = torch.empty(need, dtype=torch.uint8, device=device)
-        _tensor(out[0], "out[0]", device, (rows, k), (torch.float32,))
-        _tensor(out[1], "out[1]", device, (rows, k), (torch.int32,))
+        score = _arg(out[0], "out[0]", device, (rows, k), torch.float32)
+        index = _arg(out[1], "out[1]", device, (rows, k), torch.int32)
         _tensor(ws, "ws", device)
-        hs_topk_rows(scores, code, stride, rows, cols, k, out[0], out[1], ws, stream=stream)
+        hs_topk_rows(scores, code, stride, rows, cols, k, score, index, ws, stream=stream)
     return out
