@@ -15,7 +15,7 @@
 // Floor: dO once, dT once; the keys are small beside them.  262,144 bf16 rows of 1,024
 // columns for 131,072 tokens, fp32 gradient (1,075 MB): 268 us; the sums' launch (877 MB of
 // it) 192 us, 4.6 TB/s, a copy's rate; the sort 40 us beside zeros.  10,007 fp32 rows of 771
-// for 50,257 (186 MB): 50 us; 2,048 bf16 rows of 1,024 for 32,000 (70 MB): 25 us, of which
+// for 50,257 (186 MB): 49 us; 2,048 bf16 rows of 1,024 for 32,000 (70 MB): 25 us, of which
 // 20 are the latency of three launches, whatever zeros are written beside them.
 #include "rows.h"
 
@@ -84,7 +84,7 @@ size_t layout(int64_t n, int64_t rows, int64_t dim, void *base, GradWs *w) {
 // ---------------------------------------------------------------- rows of zeros
 //
 // The sort's launches leave most CUs idle, so further workgroups of theirs, and some of the
-// sums', write the rows of tokens that do not occur.
+// sums' and the join's, write the rows of tokens that do not occur.
 struct Zeros {
   uint8_t *table;
   int64_t first, last;    // rows that are looked at, from a multiple of 4 on
@@ -678,14 +678,18 @@ __device__ __forceinline__ void join_write(uint8_t *table, int64_t t, int c, int
 template <int OT>
 __global__ __launch_bounds__(kJoinWaves * 64) void grad_join(
     const uint32_t *__restrict__ tok, int64_t n, int64_t rows, int dim, int places,
-    int64_t chunks, float scale, int add, const uint32_t *__restrict__ count,
+    int64_t chunks, int join_blocks, float scale, int add, const uint32_t *__restrict__ count,
     const uint32_t *__restrict__ many, const float *__restrict__ part,
-    uint8_t *__restrict__ table) {
+    uint8_t *__restrict__ table, const uint8_t *__restrict__ present, Zeros z) {
   __shared__ float sums[kJoinWaves][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if ((int)blockIdx.x >= join_blocks) {
+    zero_rows(z, present, (int64_t)blockIdx.x - join_blocks, (int64_t)gridDim.x - join_blocks);
+    return;
+  }
   const int many_blocks = (dim + 63) / 64, few_blocks = (dim + 255) / 256;
   const int64_t n_many = (int64_t)*count * many_blocks, n_few = (chunks - 1) * few_blocks;
-  for (int64_t task = blockIdx.x; task < n_many; task += gridDim.x) {
+  for (int64_t task = blockIdx.x; task < n_many; task += join_blocks) {
     const int64_t e = task / many_blocks, c = many[e];
     const int col = (int)(task - e * many_blocks) * 64 + lane, cc = col < dim ? col : 0;
     const uint32_t t = tok[(c + 1) * places - 1];
@@ -712,7 +716,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void grad_join(
     __syncthreads();
   }
   for (int64_t task = (int64_t)blockIdx.x * kJoinWaves + wave; task < n_few;
-       task += (int64_t)gridDim.x * kJoinWaves) {
+       task += (int64_t)join_blocks * kJoinWaves) {
     const int64_t c = task / few_blocks;
     const int col = (int)(task - c * few_blocks) * 256 + lane;
     const uint32_t t = tok[(c + 1) * places - 1];
@@ -742,8 +746,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void grad_join(
 
 template <int DT, int OT>
 hipError_t launch_sums(const GradWs &w, int side, const void *grad, int64_t n, int64_t rows,
-                       int64_t dim, float scale, int add, void *table, const Zeros &z, int zero_wgs,
-                       hipStream_t st) {
+                       int64_t dim, float scale, int add, void *table, Zeros z, hipStream_t st) {
   constexpr int V = DT == HS_F32 ? 4 : 8;
   const int places = chunk_places(n, dim);
   const int64_t chunks = (n + places - 1) / places;
@@ -751,6 +754,20 @@ hipError_t launch_sums(const GradWs &w, int side, const void *grad, int64_t n, i
   int lanes = 1;   // that a row takes
   while (lanes < 64 && lanes * V < dim) lanes *= 2;
   const bool narrow = lanes < 64;
+  // the join's launch, short and far from the memory's rate, takes up to 24 MB of the zeros
+  // (9,000 rows of 1,000 bf16 columns, 65,536 tokens, fp32 71 -> 68 us; 37 of 300 lost 1 us,
+  // 262,144 of 1,024 2 us)
+  Zeros last = z;
+  if (n >= 512 && n <= kSmallMax) {
+    const int64_t half = (z.last - z.first) / 2, fit = (24 << 20) / (dim * z.elem);
+    z.last = z.first + (z.last - z.first - (half < fit ? half : fit)) / 4 * 4;
+  }
+  last.first = z.last;
+  auto wgs_of = [](const Zeros &r, int waves, int most) {
+    const int64_t wgs = (r.last - r.first + 4 * waves - 1) / (4 * waves);
+    return (int)(wgs < most ? wgs : most);
+  };
+  const int zero_wgs = wgs_of(z, 4, 1024);
   const int64_t sum_blocks = narrow ? (chunks * lanes + 255) / 256 : (chunks * slices + 3) / 4;
   hipLaunchKernelGGL((narrow ? grad_sums_narrow<DT, OT> : grad_sums<DT, OT>),
                      dim3((unsigned)(sum_blocks + zero_wgs)), dim3(256), 0, st,
@@ -760,9 +777,12 @@ hipError_t launch_sums(const GradWs &w, int side, const void *grad, int64_t n, i
   if (chunks > 1) {
     // (as many tasks at most, in waves)
     const int64_t tasks = ((chunks - 1) * ((dim + 255) / 256) + kJoinWaves - 1) / kJoinWaves;
-    hipLaunchKernelGGL(grad_join<OT>, dim3((unsigned)(tasks < 512 ? tasks : 512)),
-                       dim3(kJoinWaves * 64), 0, st, w.tok[side], n, rows, (int)dim, places, chunks, scale, add, w.count,
-                       w.many, w.part, (uint8_t *)table);
+    const int join_blocks = (int)(tasks < 512 ? tasks : 512);
+    hipLaunchKernelGGL(grad_join<OT>,
+                       dim3((unsigned)(join_blocks + wgs_of(last, kJoinWaves, 512))),
+                       dim3(kJoinWaves * 64), 0, st, w.tok[side], n, rows, (int)dim, places,
+                       chunks, join_blocks, scale, add, w.count, w.many, w.part,
+                       (uint8_t *)table, w.present, last);
   }
   return hipGetLastError();
 }
@@ -788,7 +808,7 @@ hipError_t launch_embed_grad(const void *grad, int grad_dtype, const void *ids, 
   const int64_t stop = add ? 0 : rows;   // rows of zeros are written below it
   const Zeros all = {(uint8_t *)table, 0, stop, (int)dim, elem};
   Zeros part[3] = {all, all, all};       // of the second count and scatter, of the sums
-  int zero_wgs[3] = {0, 0, 0};
+  int zero_wgs[2] = {0, 0};
   if (n <= kSmallMax) {
     // the sort takes about 1.6 us per 1,024 positions, in which the other CUs write some
     // 10 KiB of zeros for each; the sums' launch, short too, gets the rest
@@ -797,7 +817,6 @@ hipError_t launch_embed_grad(const void *grad, int grad_dtype, const void *ids, 
     now.last = n == 0 || fit > stop ? stop : fit;
     part[2].first = now.last;
     const int64_t zeros = part[2].last - part[2].first;
-    zero_wgs[2] = (int)((zeros + 15) / 16 < 1024 ? (zeros + 15) / 16 : 1024);
     // slabs: one workgroup for each CU but the sort's; at most as many rows as the bitmaps
     // hold
     auto slab_of = [](int64_t r) {
@@ -824,9 +843,8 @@ hipError_t launch_embed_grad(const void *grad, int grad_dtype, const void *ids, 
       part[1].last = stop * 13 / 20 / 4 * 4;
       part[2].first = part[1].last;
     }
-    for (int i = passes > 1 ? 0 : 2; i < 3; ++i) {
-      const int64_t waves = (part[i].last - part[i].first + 3) / 4;
-      const int64_t wgs = (waves + (i < 2 ? kSortWaves : 4) - 1) / (i < 2 ? kSortWaves : 4);
+    for (int i = 0; i < 2 && passes > 1; ++i) {
+      const int64_t wgs = (part[i].last - part[i].first + 4 * kSortWaves - 1) / (4 * kSortWaves);
       zero_wgs[i] = (int)(wgs < 1024 ? wgs : 1024);
     }
     const dim3 b(kSortWaves * 64);
@@ -855,14 +873,14 @@ hipError_t launch_embed_grad(const void *grad, int grad_dtype, const void *ids, 
   if (grad_dtype == HS_F32)
     return table_dtype == HS_F32
                ? launch_sums<HS_F32, HS_F32>(w, side, grad, n, rows, dim, scale, add, table,
-                                              part[2], zero_wgs[2], st)
+                                              part[2], st)
                : launch_sums<HS_F32, HS_BF16>(w, side, grad, n, rows, dim, scale, add, table,
-                                              part[2], zero_wgs[2], st);
+                                              part[2], st);
   return table_dtype == HS_F32
              ? launch_sums<HS_BF16, HS_F32>(w, side, grad, n, rows, dim, scale, add, table,
-                                              part[2], zero_wgs[2], st)
+                                              part[2], st)
              : launch_sums<HS_BF16, HS_BF16>(w, side, grad, n, rows, dim, scale, add, table,
-                                              part[2], zero_wgs[2], st);
+                                              part[2], st);
 }
 
 }  // namespace hs
