@@ -13,8 +13,8 @@
 //   join    partial sums of the tokens over several chunks, in chunk order.
 // Every row's additions are thus in an order that the sizes and ids fix.
 // Floor: dO once, dT once; the keys are small beside them.  262,144 bf16 rows of 1,024
-// columns for 131,072 tokens, fp32 gradient (1,075 MB): 268 us; the sums' launch (877 MB of
-// it) 192 us, 4.6 TB/s, a copy's rate; the sort 40 us beside zeros.  10,007 fp32 rows of 771
+// columns for 131,072 tokens, fp32 gradient (1,075 MB): 265 us; the sums' launch (877 MB of
+// it) 190 us, 4.6 TB/s, a copy's rate; the sort 40 us beside zeros.  10,007 fp32 rows of 771
 // for 50,257 (186 MB): 49 us; 2,048 bf16 rows of 1,024 for 32,000 (70 MB): 25 us, of which
 // 20 are the latency of three launches, whatever zeros are written beside them.
 #include "rows.h"
@@ -777,7 +777,7 @@ hipError_t launch_sums(const GradWs &w, int side, const void *grad, int64_t n, i
   if (chunks > 1) {
     // (as many tasks at most, in waves)
     const int64_t tasks = ((chunks - 1) * ((dim + 255) / 256) + kJoinWaves - 1) / kJoinWaves;
-    const int join_blocks = (int)(tasks < 512 ? tasks : 512);
+    const int join_blocks = (int)(tasks < 1024 ? tasks : 1024);
     hipLaunchKernelGGL(grad_join<OT>,
                        dim3((unsigned)(join_blocks + wgs_of(last, kJoinWaves, 512))),
                        dim3(kJoinWaves * 64), 0, st, w.tok[side], n, rows, (int)dim, places,
