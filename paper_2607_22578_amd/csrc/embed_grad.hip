@@ -431,7 +431,9 @@ __global__ __launch_bounds__(kSortWaves * 64) void grad_scatter(
 // ---------------------------------------------------------------- sums
 //
 // V consecutive columns per lane and slice.  A row's last lane takes the last V columns,
-// some of them its neighbour's too: both get the same sums, in the same instructions.
+// some of them the lane before's too (of another wave, where it is the first lane of its
+// slice): both get the same sums and store the same values, but where sums are added to what
+// the table holds, one of them alone may do it (see write).
 // Rows of less than V columns are one lane's.
 template <int DT>
 struct Slice {
@@ -480,10 +482,18 @@ struct Slice {
 #pragma unroll
       for (int j = 0; j < V; ++j) o[j] = v[j] * scale;
       if (add) {
+        // (columns below a multiple of V are the lane before's, which reads and writes them
+        // by itself, in whatever wave it is)
+        const int own = (c + V - 1) / V * V;
+        if (own > c) {
+#pragma unroll
+          for (int j = 1; j < V; ++j)
+            if (c + j >= own) store_col<OT>(row, c + j, o[j] + load_col<OT>(row, c + j));
+          return;
+        }
         RawCols<OT, V> raw;
         float old[V];
         raw.load(row, c);
-        wave_fence();   // (the last lane's neighbour reads some of its columns: before any store)
         raw.decode(old);
 #pragma unroll
         for (int j = 0; j < V; ++j) o[j] += old[j];

@@ -175,6 +175,26 @@ def test_embed_grad_accumulate_and_padding(dim, dout):
     run_grad(rng, 50, 40, dim, F32, dout, ids=np.full(50, 40))
 
 
+@pytest.mark.parametrize("din,dim", [
+    (F32, 255), (F32, 257), (F32, 258), (F32, 259), (F32, 771), (F32, 1025), (F32, 2049),
+    (BF16, 511), (BF16, 513), (BF16, 515), (BF16, 519), (BF16, 1025), (BF16, 2049)])
+@pytest.mark.parametrize("dout", [F32, BF16])
+def test_embed_grad_accumulates_each_column_once(din, dim, dout):
+    """Widths whose last columns are fewer than a lane's, many of them where the row's last
+    lane is in another wave than the one before: tokens that occur once, over a few and
+    over many chunks."""
+    rng = np.random.default_rng(dim)
+    lengths = [1] * 300 + [2, 9, 40, 100, 300, 700]
+    ids = rng.permutation(np.repeat(np.arange(len(lengths)), lengths))
+    d, _, _ = run_grad(rng, len(ids), len(lengths) + 3, dim, din, dout, ids=ids, accumulate=True)
+    args = (d.to(device()), torch.from_numpy(ids).to(device()), len(lengths) + 3)
+    plain = hs.embed_grad(*args, out_dtype=dout)
+    for _ in range(3):     # added to zeros: the plain gradient
+        out = torch.zeros_like(plain)
+        hs.embed_grad(*args, out=out, accumulate=True)
+        assert torch.equal(out, plain)
+
+
 @pytest.mark.parametrize("n", [1, 100, 4096, 30_000])
 def test_embed_grad_one_token_and_all_distinct(n):
     rng = np.random.default_rng(n)
