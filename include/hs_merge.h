@@ -447,9 +447,11 @@ hs_status hs_embed(const hs_row_table *table, const void *ids, int32_t ids_is_i6
  * (accumulate = 1: are left untouched).
  *   d_out    [n x dim] device, HS_F32 or HS_BF16
  *   d_table  [rows x dim] device, HS_F32 or HS_BF16: out (accumulate = 0) or in and
- *            out (1).  Both aligned to their elements; must not overlap
- *   ws       device, 256-byte aligned, of hs_embed_grad_bytes' size; every call writes
- *            what it reads of it, so calls may share one unless they overlap in time */
+ *            out (1).  Both aligned to their elements; must not overlap each other, nor
+ *            d_table the ids
+ *   ws       device, 256-byte aligned, of hs_embed_grad_bytes' size, apart from all
+ *            others; every call writes what it reads of it, so calls may share one unless
+ *            they overlap in time */
 hs_status hs_embed_grad_bytes(int64_t n, int64_t rows, int64_t dim, size_t *bytes);
 hs_status hs_embed_grad(const void *d_out, int32_t d_out_dtype, const void *ids,
                         int32_t ids_is_i64, int64_t n, int64_t rows, int64_t dim, float scale,

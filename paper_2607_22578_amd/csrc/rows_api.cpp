@@ -204,9 +204,18 @@ hs_status hs_embed_grad(const void *d_out, int32_t d_out_dtype, const void *ids,
     return fail(HS_ERR_WORKSPACE, "%s: workspace %zu bytes, need %zu", who, ws_bytes, need);
   if (!aligned(ws, 256))
     return fail(HS_ERR_ALIGNMENT, "%s: workspace must be 256-byte aligned", who);
-  if (overlap(d_out, (uint64_t)n * (uint64_t)dim * elem(d_out_dtype), d_table,
-              (uint64_t)rows * (uint64_t)dim * elem(d_table_dtype)))
+  const uint64_t gb = (uint64_t)n * (uint64_t)dim * elem(d_out_dtype),
+                 tb = (uint64_t)rows * (uint64_t)dim * elem(d_table_dtype),
+                 ib = (uint64_t)n * (ids_is_i64 ? 8 : 4);
+  if (overlap(d_out, gb, d_table, tb))
     return fail(HS_ERR_INVALID_ARG, "%s: d_out and d_table overlap", who);
+  // (a call that writes nothing writes nothing of its workspace either)
+  if (rows > 0 && (n > 0 || !accumulate)) {
+    if (overlap(ids, ib, d_table, tb))
+      return fail(HS_ERR_INVALID_ARG, "%s: ids and d_table overlap", who);
+    if (overlap(ws, need, d_out, gb) || overlap(ws, need, ids, ib) || overlap(ws, need, d_table, tb))
+      return fail(HS_ERR_INVALID_ARG, "%s: the workspace overlaps d_out, ids or d_table", who);
+  }
   return device_status(hs::launch_embed_grad(d_out, d_out_dtype, ids, ids_is_i64, n, rows, dim,
                                              scale, pad_id, accumulate, d_table, d_table_dtype,
                                              ws, (hipStream_t)stream),

@@ -104,6 +104,29 @@ def test_embed_grad():
     hs.hs_embed_grad(None, hs.HS_F32, None, 0, 0, 9, 8, 1.0, -1, 1, FAKE, hs.HS_F32, FAKE, 1 << 30)
 
 
+@pytest.mark.parametrize("accumulate", [0, 1])
+def test_embed_grad_overlaps(accumulate):
+    """The sort's launch writes rows of zeros while others still read ids, and the
+    workspace all along: neither may lie on what the call reads or writes."""
+    need = hs.hs_embed_grad_bytes(100, 50, 64)
+    good = [FAKE, hs.HS_BF16, BIG, 0, 100, 50, 64, 1.0, -1, accumulate, 2 * BIG, hs.HS_F32,
+            3 * BIG, need]
+    for at, bad in [(2, 2 * BIG), (2, 2 * BIG + 50 * 64 * 4 - 4), (2, 2 * BIG - 396),   # ids
+                    (12, FAKE), (12, FAKE + 100 * 64 * 2 - 256), (12, BIG), (12, BIG + 256),
+                    (12, 2 * BIG), (12, 2 * BIG + 50 * 64 * 4 - 256),                   # ws
+                    (10, 3 * BIG + need - 4), (0, 3 * BIG + need - 2), (2, 3 * BIG + need - 4)]:
+        args = list(good)
+        args[at] = bad
+        refused(INVALID, hs.hs_embed_grad, *args)
+    # int64 ids reach twice as far
+    args = list(good)
+    args[2], args[3] = 2 * BIG - 800 + 8, 1
+    refused(INVALID, hs.hs_embed_grad, *args)
+    # (a table of no rows, or nothing to add: the call writes nothing)
+    hs.hs_embed_grad(FAKE, hs.HS_F32, FAKE, 0, 9, 0, 8, 1.0, -1, accumulate, None, hs.HS_F32, FAKE,
+                     1 << 30)
+
+
 def test_score_packed():
     t = table()
     good = [t, 2 * BIG, hs.HS_F32, 4, 3 * BIG, hs.HS_F32, 1000]
