@@ -521,8 +521,8 @@ hs_status hs_adjust_scores(const hs_adjust *adjust, const void *scores, int64_t 
  *   k           1 <= k <= 1024 (k > n_cols pads)
  *   topk_score  [n_rows x k] fp32 device out
  *   topk_index  [n_rows x k] int32 device out; neither overlaps scores or the other
- *   ws          device, 256-byte aligned, of hs_topk_rows_bytes' size; every call
- *               writes what it reads of it
+ *   ws          device, 256-byte aligned, of hs_topk_rows_bytes' size, apart from
+ *               scores and outputs; every call writes what it reads of it
  * Bit-exact and deterministic.  (Rows with thousands of scores equal to the k-th best
  * take several passes over them.) */
 hs_status hs_topk_rows_bytes(int64_t n_rows, int64_t n_cols, int32_t k, size_t *bytes);

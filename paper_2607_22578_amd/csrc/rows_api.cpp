@@ -334,19 +334,22 @@ hs_status hs_topk_rows(const void *scores, int32_t dtype, int64_t stride, int64_
     return fail(HS_ERR_INVALID_ARG, "%s: null output", who);
   if (!aligned(topk_score, 4) || !aligned(topk_index, 4))
     return fail(HS_ERR_ALIGNMENT, "%s: misaligned output", who);
-  if (n_rows > 0 && n_cols > 0) {
-    const uint64_t sb = ((uint64_t)(n_rows - 1) * (uint64_t)stride + (uint64_t)n_cols) *
-                        elem(dtype),
-                   kb = (uint64_t)n_rows * (uint64_t)k * 4;
-    if (overlap(scores, sb, topk_score, kb) || overlap(scores, sb, topk_index, kb) ||
-        overlap(topk_score, kb, topk_index, kb))
-      return fail(HS_ERR_INVALID_ARG, "%s: scores and the outputs overlap", who);
-  }
+  const uint64_t sb = n_rows > 0 && n_cols > 0
+                          ? ((uint64_t)(n_rows - 1) * (uint64_t)stride + (uint64_t)n_cols) *
+                                elem(dtype)
+                          : 0,
+                 kb = (uint64_t)n_rows * (uint64_t)k * 4;
+  if (overlap(scores, sb, topk_score, kb) || overlap(scores, sb, topk_index, kb) ||
+      overlap(topk_score, kb, topk_index, kb))
+    return fail(HS_ERR_INVALID_ARG, "%s: scores and the outputs overlap", who);
   const size_t need = hs::topk_rows_workspace_bytes(n_rows, n_cols, k);
   if (!ws || ws_bytes < need)
     return fail(HS_ERR_WORKSPACE, "%s: workspace %zu bytes, need %zu", who, ws_bytes, need);
   if (!aligned(ws, 256))
     return fail(HS_ERR_ALIGNMENT, "%s: workspace must be 256-byte aligned", who);
+  if (n_rows > 0 && (overlap(ws, need, scores, sb) || overlap(ws, need, topk_score, kb) ||
+                     overlap(ws, need, topk_index, kb)))
+    return fail(HS_ERR_INVALID_ARG, "%s: the workspace overlaps scores or an output", who);
   return device_status(hs::launch_topk_rows(scores, dtype, stride, n_rows, n_cols, k, topk_score,
                                             topk_index, ws, (hipStream_t)stream),
                        "hs_topk_rows launch");

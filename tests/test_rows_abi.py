@@ -197,6 +197,19 @@ def test_topk_rows():
     hs.hs_topk_rows(None, hs.HS_F32, 10, 0, 10, 5, None, None, FAKE, 1 << 20)
 
 
+def test_topk_rows_workspace_overlaps():
+    """The maxima are written while scores are still read; the outputs while maxima are."""
+    need = hs.hs_topk_rows_bytes(4, 100_000, 50)
+    good = [FAKE, hs.HS_F32, 100_000, 4, 100_000, 50, BIG, 2 * BIG, 3 * BIG, need]
+    for at, bad in [(8, FAKE), (8, FAKE + 1_600_000 - 256), (8, BIG), (8, BIG + 512),
+                    (8, 2 * BIG), (0, 3 * BIG + need - 4), (6, 3 * BIG + need - 4),
+                    (7, 3 * BIG + need - 4)]:
+        args = list(good)
+        args[at] = bad
+        refused(INVALID, hs.hs_topk_rows, *args)
+    hs.hs_topk_rows(FAKE, hs.HS_F32, 10, 0, 10, 5, FAKE, FAKE, FAKE, 1 << 20)   # (no rows)
+
+
 def test_python_functions_refuse():
     """The one-call functions' own checks (CPU tensors: no device call is reached)."""
     f = torch.zeros(4, 64)
