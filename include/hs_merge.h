@@ -508,6 +508,8 @@ typedef struct {
  *               elements, each with its own stride >= n_cols (elements; columns
  *               from n_cols on are left as they were); out may be scores itself
  *               (same stride), else the two must not overlap
+ *               (The columns of out that are written must not lie on a list, an array or
+ *               a mask.)
  * 0 <= n_rows <= 2^20, 0 <= n_cols <= 2^31 - 1; n_rows * n_cols <= 2^40. */
 hs_status hs_adjust_scores(const hs_adjust *adjust, const void *scores, int64_t stride, void *out,
                            int64_t out_stride, int32_t dtype, int64_t n_rows, int64_t n_cols,

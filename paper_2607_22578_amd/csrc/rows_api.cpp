@@ -43,6 +43,18 @@ static bool overlap(const void *a, uint64_t an, const void *b, uint64_t bn) {
   return an > 0 && bn > 0 && x < y + bn && y < x + an;
 }
 
+// The same for n rows of `row` bytes that start `step` >= row bytes apart: what lies between
+// them does not count.
+static bool on_rows(const void *rows, uint64_t row, uint64_t step, int64_t n, const void *b,
+                    uint64_t bn) {
+  if (n <= 0 || !overlap(rows, (uint64_t)(n - 1) * step + row, b, bn)) return false;
+  const uint64_t x = (uint64_t)(uintptr_t)rows, y = (uint64_t)(uintptr_t)b;
+  const uint64_t i = y > x ? (y - x) / step : 0;   // the last row that starts at b or before
+  return overlap(b, bn, (const void *)(uintptr_t)(x + i * step), row) ||
+         (i + 1 < (uint64_t)n &&
+          overlap(b, bn, (const void *)(uintptr_t)(x + (i + 1) * step), row));
+}
+
 static hs_status check_shape(int64_t rows, int64_t dim, const char *who) {
   if (rows < 0 || rows > kRowsMax)
     return fail(HS_ERR_INVALID_ARG, "%s: rows %lld out of [0, 2^31-1]", who, (long long)rows);
@@ -294,6 +306,26 @@ hs_status hs_adjust_scores(const hs_adjust *adjust, const void *scores, int64_t 
       !aligned(a.presence, 4) || !aligned(a.bias_id, 4) || !aligned(a.bias, 4) ||
       !aligned(a.allow, 4))
     return fail(HS_ERR_ALIGNMENT, "%s: misaligned list or array", who);
+  if (n_rows > 0 && n_cols > 0) {
+    const uint64_t row = (uint64_t)n_cols * elem(dtype), step = (uint64_t)out_stride * elem(dtype),
+                   n = (uint64_t)n_rows, words = ((uint64_t)n_cols + 31) / 32;
+    auto on_out = [&](const void *p, uint64_t bytes) {
+      return p && on_rows(out, row, step, n_rows, p, bytes);
+    };
+    bool on = on_out(a.prompt_len, n * 4) || on_out(a.repetition, n * 4) ||
+              on_out(a.frequency, n * 4) || on_out(a.presence, n * 4);
+    if (a.seen_off)
+      on = on || on_out(a.seen_off, (n + 1) * 8) || on_out(a.seen, (uint64_t)a.n_seen * 4);
+    if (a.bias_off)
+      on = on || on_out(a.bias_off, (n + 1) * 8) || on_out(a.bias_id, (uint64_t)a.n_bias * 4) ||
+           on_out(a.bias, (uint64_t)a.n_bias * 4);
+    // (the masks may lie between the rows, one behind each: looked at one by one if so)
+    const uint64_t masks = a.allow && a.allow_stride > 0 ? n : 1;
+    if (on_out(a.allow, ((masks - 1) * (uint64_t)a.allow_stride + words) * 4))
+      for (uint64_t r = 0; r < masks && !on; ++r)
+        on = on_out(a.allow + r * (uint64_t)a.allow_stride, words * 4);
+    if (on) return fail(HS_ERR_INVALID_ARG, "%s: out overlaps a list, an array or a mask", who);
+  }
   if (n_rows > 0 && n_cols > 0 && !(scores == out && stride == out_stride)) {
     const uint64_t es = elem(dtype);
     const uint64_t ib = ((uint64_t)(n_rows - 1) * (uint64_t)stride + (uint64_t)n_cols) * es,

@@ -175,6 +175,58 @@ def test_adjust_scores():
     hs.hs_adjust_scores(adjust(), None, 0, None, 0, hs.HS_BF16, 5, 0)
 
 
+LISTS = ["seen_off", "seen", "prompt_len", "repetition", "frequency", "presence", "bias_off",
+         "bias_id", "bias", "allow"]
+
+
+def lists(**kw):
+    """All lists and arrays of four rows (100 columns), each BIG apart from the others."""
+    base = {n: (10 + i) * BIG for i, n in enumerate(LISTS)}
+    base.update(n_seen=30, n_bias=20, allow_stride=4)
+    base.update(kw)
+    return adjust(**base)
+
+
+@pytest.mark.parametrize("name,size", [
+    ("seen_off", 40), ("seen", 120), ("prompt_len", 16), ("repetition", 16), ("frequency", 16),
+    ("presence", 16), ("bias_off", 40), ("bias_id", 80), ("bias", 80), ("allow", 64)])
+def test_adjust_scores_overlaps(name, size):
+    """Other workgroups still read the lists, arrays and masks while out is written."""
+    # out: four rows of 400 bytes, 512 apart
+    for at in (BIG, BIG + 392, BIG + 512, BIG + 3 * 512 + 392, BIG - size + 8):
+        for scores in (FAKE, BIG):                     # (out of place and in place)
+            refused(INVALID, hs.hs_adjust_scores, lists(**{name: at}), scores, 128, BIG, 128,
+                    hs.HS_F32, 4, 100)
+
+
+def accepted(call, *args):
+    """Validation passes: what fails, without a GPU, is the device call behind it."""
+    try:
+        call(*args)
+    except hs.HsError as e:
+        assert e.status == hs.HS_ERR_DEVICE, hs.hs_last_error()
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="would launch on made-up addresses")
+@pytest.mark.parametrize("name,size", [("seen_off", 40), ("bias", 80), ("allow", 64)])
+def test_adjust_scores_between_rows(name, size):
+    """Lists before, behind and between the rows of out; a mask of each row behind its
+    scores; lists of no entries anywhere."""
+    rows = [hs.HS_F32, 4, 100]
+    for at in (BIG - size, BIG + 3 * 512 + 400, BIG + 400):
+        a = lists(**{name: at})
+        accepted(hs.hs_adjust_scores, a, FAKE, 128, BIG, 128, *rows)
+    a = lists(allow=BIG + 400, allow_stride=128)
+    accepted(hs.hs_adjust_scores, a, BIG, 128, BIG, 128, *rows)
+    a = lists(seen=BIG, n_seen=0)
+    accepted(hs.hs_adjust_scores, a, BIG, 128, BIG, 128, *rows)
+    # (a mask of 4 words a row, one word too far to the front)
+    refused(INVALID, hs.hs_adjust_scores, lists(allow=BIG + 396, allow_stride=128), BIG, 128, BIG,
+            128, *rows)
+    refused(INVALID, hs.hs_adjust_scores, lists(allow=BIG + 400, allow_stride=127), BIG, 128, BIG,
+            128, *rows)
+
+
 def test_topk_rows():
     need = hs.hs_topk_rows_bytes(4, 100_000, 50)
     assert need >= 256
