@@ -379,8 +379,10 @@ hs_status hs_topk_rows(const void *scores, int32_t dtype, int64_t stride, int64_
     return fail(HS_ERR_WORKSPACE, "%s: workspace %zu bytes, need %zu", who, ws_bytes, need);
   if (!aligned(ws, 256))
     return fail(HS_ERR_ALIGNMENT, "%s: workspace must be 256-byte aligned", who);
-  if (n_rows > 0 && (overlap(ws, need, scores, sb) || overlap(ws, need, topk_score, kb) ||
-                     overlap(ws, need, topk_index, kb)))
+  if (n_rows > 0 &&
+      (on_rows(scores, (uint64_t)n_cols * elem(dtype), (uint64_t)stride * elem(dtype), n_rows, ws,
+               need) ||
+       overlap(ws, need, topk_score, kb) || overlap(ws, need, topk_index, kb)))
     return fail(HS_ERR_INVALID_ARG, "%s: the workspace overlaps scores or an output", who);
   return device_status(hs::launch_topk_rows(scores, dtype, stride, n_rows, n_cols, k, topk_score,
                                             topk_index, ws, (hipStream_t)stream),

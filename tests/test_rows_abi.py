@@ -262,6 +262,17 @@ def test_topk_rows_workspace_overlaps():
     hs.hs_topk_rows(FAKE, hs.HS_F32, 10, 0, 10, 5, FAKE, FAKE, FAKE, 1 << 20)   # (no rows)
 
 
+@pytest.mark.skipif(torch.cuda.is_available(), reason="would launch on made-up addresses")
+def test_topk_rows_workspace_between_rows():
+    """A workspace in what follows the columns of a row of scores."""
+    need = hs.hs_topk_rows_bytes(4, 10_000, 50)
+    assert need == 256
+    args = [BIG, hs.HS_F32, 12_032, 4, 10_000, 50, 2 * BIG, 3 * BIG, BIG + 40_192, need]
+    accepted(hs.hs_topk_rows, *args)
+    args[8] = BIG + 48_128      # the second row's first columns
+    refused(INVALID, hs.hs_topk_rows, *args)
+
+
 def test_python_functions_refuse():
     """The one-call functions' own checks (CPU tensors: no device call is reached)."""
     f = torch.zeros(4, 64)
