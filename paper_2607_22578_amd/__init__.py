@@ -600,27 +600,33 @@ class MergedRetrieval:
         group is that of its first request).  Reads the distinct count on the host (one
         synchronisation).  A request with fewer than k allowed chunks has (-inf, -1) in
         the slots left."""
+        if table.c.dtype != HS_FP4_E2M1:
+            raise TypeError("the table must be packed (pack_rows)")
         if (table.rows, table.dim) != (self.N, self.d):
             raise ValueError(f"a table of {table.rows} x {table.dim} for a corpus of "
                              f"{self.N} x {self.d}")
+        dev = self.ws.device
+        if table.device != dev:
+            raise ValueError(f"table is on {table.device}, not on {dev}")
+        words = (self.N + 31) // 32
+        if allow is not None and words > 0:
+            if tuple(allow.shape) not in ((words,), (self.R, words)):
+                raise ValueError(f"allow has shape {tuple(allow.shape)}, not ({words},) or "
+                                 f"({self.R}, {words})")
+            _tensor(allow, "allow", dev, dtypes=(_torch.int32,))
         if not hasattr(self, "packed_scores"):
             self.enable_packed()
             # (`stream` must not overtake what still uses the memory just taken)
-            _torch.cuda.current_stream(self.ws.device).synchronize()
-        words = (self.N + 31) // 32
+            _torch.cuda.current_stream(dev).synchronize()
         if allow is not None and allow.dim() == 2 and self.packed_allow is None:
             self.packed_allow = _torch.empty((self.packed_batch, max(words, 1)),
-                                             dtype=_torch.int32, device=self.ws.device)
-            _torch.cuda.current_stream(self.ws.device).synchronize()
+                                             dtype=_torch.int32, device=dev)
+            _torch.cuda.current_stream(dev).synchronize()
         nu = self.dedup(keys, stream, host_count=True)
         hs_scatter(q_req, self.R, self.q_row_bytes, self.first_index, 0, self.R, self.n_unique,
                    self.q_unique, stream=stream)
         adj = hs_adjust()
         if allow is not None and words > 0:
-            if tuple(allow.shape) not in ((words,), (self.R, words)):
-                raise ValueError(f"allow has shape {tuple(allow.shape)}, not ({words},) or "
-                                 f"({self.R}, {words})")
-            _tensor(allow, "allow", self.ws.device, dtypes=(_torch.int32,))
             adj.allow = _ptr(allow)
             if allow.dim() == 2:
                 adj.allow = _ptr(self.packed_allow)

@@ -273,6 +273,40 @@ def test_topk_rows_workspace_between_rows():
     refused(INVALID, hs.hs_topk_rows, *args)
 
 
+def test_run_packed_refuses_before_it_begins(monkeypatch):
+    """A table or masks that do not fit are found before anything is enqueued or made."""
+    m = hs.MergedRetrieval(6, 64, 100, 3, hs.HS_F32, hs.HS_F32, device="cpu")
+
+    def begun(*args, **kw):
+        raise AssertionError("the window has begun")
+
+    for name in ("hs_dedup", "hs_scatter", "hs_score_packed", "hs_deliver"):
+        monkeypatch.setattr(hs, name, begun)
+    keys, q = torch.zeros(6, dtype=torch.int64), torch.zeros(6, 64)
+
+    def table(rows=100, dim=64, device="cpu"):
+        return hs.RowTable(torch.zeros(rows, dim // 2, dtype=torch.uint8, device=device),
+                           torch.zeros(rows, dim // 32, device=device), group=32)
+
+    def words(*shape, dtype=torch.int32, device="cpu"):
+        return torch.zeros(shape, dtype=dtype, device=device)
+
+    t = table()
+    for bad, err in [((table(rows=99),), ValueError), ((table(dim=96),), ValueError),
+                     ((table(device="meta"),), ValueError),
+                     ((hs.RowTable(torch.zeros(100, 64)),), TypeError),
+                     ((hs.RowTable(torch.zeros(100, 64, dtype=torch.uint8), torch.zeros(100)),),
+                      TypeError),
+                     ((t, words(3)), ValueError), ((t, words(5, 4)), ValueError),
+                     ((t, words(6, 5)), ValueError), ((t, words(1, 6, 4)), ValueError),
+                     ((t, words(4, dtype=torch.int64)), TypeError),
+                     ((t, words(4, device="meta")), ValueError),
+                     ((t, words(4, 6).t()), ValueError)]:
+        with pytest.raises(err):
+            m.run_packed(keys, q, *bad)
+        assert not hasattr(m, "packed_scores")
+
+
 def test_python_functions_refuse():
     """The one-call functions' own checks (CPU tensors: no device call is reached)."""
     f = torch.zeros(4, 64)
