@@ -477,20 +477,14 @@ struct Slice {
                                                float scale, int add, const float *v) {
     constexpr int OB = OT == HS_F32 ? 4 : 2;
     uint8_t *row = table + r * (int64_t)dim * OB;
-    if (c + V <= dim) {
+    // (added to, columns below a multiple of V are the lane before's, which reads and writes
+    // them by itself, in whatever wave it is)
+    const int own = add ? (c + V - 1) / V * V : c;
+    if (c + V <= dim && own == c) {
       float o[V];
 #pragma unroll
       for (int j = 0; j < V; ++j) o[j] = v[j] * scale;
       if (add) {
-        // (columns below a multiple of V are the lane before's, which reads and writes them
-        // by itself, in whatever wave it is)
-        const int own = (c + V - 1) / V * V;
-        if (own > c) {
-#pragma unroll
-          for (int j = 1; j < V; ++j)
-            if (c + j >= own) store_col<OT>(row, c + j, o[j] + load_col<OT>(row, c + j));
-          return;
-        }
         RawCols<OT, V> raw;
         float old[V];
         raw.load(row, c);
@@ -511,7 +505,7 @@ struct Slice {
     } else {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        if (c + j >= dim) continue;
+        if (c + j < own || c + j >= dim) continue;
         const float o = v[j] * scale;
         store_col<OT>(row, c + j, add ? o + load_col<OT>(row, c + j) : o);
       }
