@@ -461,8 +461,9 @@ hs_status hs_embed_grad(const void *d_out, int32_t d_out_dtype, const void *ids,
 /* Products of a few rows with every row of a packed table (an output head for
  * single tokens; the scores of few queries over a 4-bit corpus):
  *   out[m][r] = sum over groups g of scale[r][g] * sum_{c in g} x[m][c] * code[r][c]
- * Products are exact (fp32 x in three bf16 parts), sums in fp32, one rounding to
- * out_dtype.  Equal table rows get bit-identical scores.
+ * Products are exact (fp32 x in three bf16 parts: magnitudes below 2^-110 lose what of
+ * them lies under 2^-133, bf16's least value), sums in fp32, one rounding to out_dtype.
+ * Equal table rows get bit-identical scores.
  *   table      an HS_FP4_E2M1 table
  *   x          [n_x x dim] device, HS_F32 or HS_BF16, 16-byte aligned; 0 <= n_x <= 2^20
  *              (finite: a NaN or infinity in row m makes out[m] NaN or infinite)

@@ -6,7 +6,9 @@
 // products run on the bf16 matrix cores: mfma_f32_16x16x32_bf16 with 16 rows of x as
 // the left and 16 table rows as the right operand.  The sums of one group are scaled
 // and added in fp32.  fp32 rows of x are split into three bf16 parts (the top 8, the
-// next 8 and the last 8 significant bits: exact).
+// next 8 and the last 8 significant bits: exact from 2^-110 on; of smaller values the bits
+// below bf16's least, 2^-133, are left out.  The matrix cores take subnormal parts as they
+// are).
 //
 // A wave takes 256 columns of its table rows at a time: lane l has row l % 16 and the
 // 32 bytes (64 columns) l / 16 of the 128, so each row's segment is a whole cache
@@ -232,7 +234,7 @@ struct Block {
 
 // Stages columns [c0, c0 + cols) of rows [m0, m0 + m) of x in LDS, zeros past the
 // last column; fp32 as three bf16 parts (truncated, so that nothing overflows; each
-// rest is exact).  cols is a multiple of 8.
+// rest is exact, and 0 below 2^-133).  cols is a multiple of 8.
 template <int XT>
 __device__ __forceinline__ void stage_x(const uint8_t *x, int64_t m0, int m, int dim, int c0,
                                         int cols, int row_bytes, int part_bytes, uint8_t *lds) {

@@ -89,6 +89,27 @@ def test_score_packed_fp32_rows_keep_their_bits():
     assert torch.equal(got, x.sum(1, keepdim=True).expand(40, 16))
 
 
+def test_score_packed_fp32_rows_near_the_least_values():
+    """The three parts end at bf16's least value, 2^-133: fp32 values from 2^-110 on keep
+    their 24 bits, smaller ones lose what lies below it; bf16 rows lose nothing."""
+    rng = np.random.default_rng(5)
+    v = ((1 + rng.random(400)) * 2.0 ** rng.integers(-149, -90, 400)).astype(np.float32)
+    v[::2] *= -1
+    x = torch.zeros(400, 32)
+    x[torch.arange(400), torch.arange(400) % 32] = torch.from_numpy(v)
+    codes = torch.full((16, 16), 0x22, dtype=torch.uint8, device=device())      # all codes 1.0
+    for scale in (1.0, 2.0 ** 100):
+        table = hs.RowTable(codes, torch.full((16, 1), scale, device=device()), group=32)
+        got = ref.f64(hs.score_packed(table, x.to(device())))[:, 0]
+        want = v.astype(np.float64) * scale
+        whole = np.abs(v) >= 2.0 ** -110
+        np.testing.assert_array_equal(got[whole], want[whole])
+        assert (np.abs(got - want) < 2.0 ** -133 * scale).all()
+        b = x.to(BF16)
+        got = ref.f64(hs.score_packed(table, b.to(device())))[:, 0]
+        np.testing.assert_array_equal(got, ref.f64(b).sum(axis=1) * scale)
+
+
 def test_score_packed_strided_out_and_equal_rows():
     rng = np.random.default_rng(6)
     table, values = packed_table(rng, 333, 256, 64, BF16)
@@ -473,4 +494,3 @@ def test_streams_and_two_calls_at_once():
         torch.cuda.synchronize(dev)
         for a, b in zip(got, want):
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
-
