@@ -288,6 +288,52 @@ def test_adjust_offsets_are_clamped():
     assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(300, 40_001), (130, 40_007), (2, 3001)])
+def test_adjust_more_marked_columns_than_the_table_holds(dtype, rows, cols):
+    """Ranges of columns with more than 1,536 seen or biased ones are taken in pieces:
+    marks over the whole row, in the second half of its first range, at its end, in one list
+    and in both, entries in any order, some of them again and again."""
+    rng = np.random.default_rng(cols)
+    dev = device()
+    width = min(10_240, cols)
+    regions = [(0, cols, 0.9), (width // 2, width, 1.0), (0, width, 0.25), (cols - 4000, cols, 0.8),
+               (0, cols, 0.05)]
+
+    def entries():
+        off, ids = [0], []
+        for r in range(rows):
+            if r < 2 * len(regions):
+                lo, hi, p = regions[r % len(regions)]
+                lo = max(lo, 0)
+                c = rng.permutation(np.flatnonzero(rng.random(hi - lo) < p) + lo)
+                c = np.concatenate([c, rng.choice(c, len(c) // 3), [-1, cols]])
+            else:
+                c = rng.integers(0, cols, rng.integers(0, 40))
+            ids.append(c)
+            off.append(off[-1] + len(c))
+        return np.concatenate(ids).astype(np.int32), np.array(off, dtype=np.int64)
+
+    seen, seen_off = entries()
+    bias_id, bias_off = entries()
+    ok = rng.random((rows, cols)) < 0.8
+    rk = dict(seen=seen, seen_off=seen_off, bias_id=bias_id, bias_off=bias_off,
+              bias=(5 * rng.standard_normal(len(bias_id))).astype(np.float32),
+              prompt_len=(rng.random(rows) * np.diff(seen_off)).astype(np.int32),
+              repetition=(0.5 + rng.random(rows)).astype(np.float32),
+              frequency=rng.standard_normal(rows).astype(np.float32),
+              presence=rng.standard_normal(rows).astype(np.float32))
+    kw = {n: torch.from_numpy(v).to(dev) for n, v in rk.items()}
+    scores = torch.from_numpy((4 * rng.standard_normal((rows, cols))).astype(np.float32)).to(dtype)
+    want, mag = ref.adjust(ref.f64(scores), allow=ok, **rk)
+    dev_scores = scores.to(dev)
+    got = hs.adjust_scores(dev_scores, allow=ref.mask_words(ok).to(dev), **kw)
+    # (at most six roundings of values that the magnitudes bound)
+    ref.check(got, want, 8 * 2.0 ** -24 * np.where(np.isfinite(mag), mag, 0.0), dtype)
+    hs.adjust_scores(dev_scores, allow=ref.mask_words(ok).to(dev), out=dev_scores, **kw)
+    assert torch.equal(dev_scores, got)
+
+
 # ------------------------------------------------------------------ top-k
 
 def check_topk(scores, k):
@@ -494,3 +540,39 @@ def test_streams_and_two_calls_at_once():
         torch.cuda.synchronize(dev)
         for a, b in zip(got, want):
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_each_operator_twice_at_once():
+    """The other operators on two streams at once, each call with tensors (and a workspace)
+    of its own: results as alone."""
+    dev = device()
+    rng = np.random.default_rng(43)
+    calls = []
+    for i in range(2):
+        table, _ = packed_table(rng, 20_000, 512, 64, BF16)
+        x = torch.from_numpy(rng.standard_normal((7 + 20 * i, 512)).astype(np.float32)).to(dev)
+        ids = torch.from_numpy(rng.integers(-1, 20_000, 9000 + 9000 * i)).to(dev)
+        d = torch.from_numpy(rng.standard_normal((len(ids), 130)).astype(np.float32)).to(dev)
+        s = torch.from_numpy(rng.standard_normal((9, 30_000)).astype(np.float32)).to(dev)
+        seen = torch.from_numpy(rng.integers(0, 30_000, 9 * 50).astype(np.int32)).to(dev)
+        off = torch.arange(10, device=dev) * 50
+        pen = torch.ones(9, device=dev)
+        w = torch.from_numpy(rng.standard_normal((3000, 256)).astype(np.float32)).to(dev)
+        calls.append([
+            lambda st, t=table, i=ids: hs.embed(t, i, scale=3.0, stream=st),
+            lambda st, i=ids, d=d: hs.embed_grad(d, i, 20_000, stream=st),
+            lambda st, t=table, x=x: hs.score_packed(t, x, stream=st),
+            lambda st, s=s, i=seen, o=off, p=pen: hs.adjust_scores(
+                s, seen=i, seen_off=o, frequency=p, stream=st),
+            lambda st, w=w: hs.pack_rows(w, group=64, stream=st).data])
+    want = [[call(None) for call in side] for side in calls]
+    torch.cuda.synchronize(dev)
+    streams = [torch.cuda.Stream(dev) for _ in range(2)]
+    for _ in range(3):
+        got = [[], []]
+        for pair in zip(*calls):
+            for call, st, to in zip(pair, streams, got):
+                to.append(call(st))
+        torch.cuda.synchronize(dev)
+        for a, b in zip(got, want):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
