@@ -526,8 +526,9 @@ hs_status hs_adjust_scores(const hs_adjust *adjust, const void *scores, int64_t 
  *   topk_index  [n_rows x k] int32 device out; neither overlaps scores or the other
  *   ws          device, 256-byte aligned, of hs_topk_rows_bytes' size, apart from
  *               scores and outputs; every call writes what it reads of it
- * Bit-exact and deterministic.  (Rows with thousands of scores equal to the k-th best
- * take several passes over them.) */
+ * Bit-exact and deterministic.  (Where thousands of scores equal the k-th best, they are
+ * looked for from column 0 on by the row's one workgroup: 24 rows of 1M whose ties lie at the
+ * end take twenty times as long as others.) */
 hs_status hs_topk_rows_bytes(int64_t n_rows, int64_t n_cols, int32_t k, size_t *bytes);
 hs_status hs_topk_rows(const void *scores, int32_t dtype, int64_t stride, int64_t n_rows,
                        int64_t n_cols, int32_t k, float *topk_score, int32_t *topk_index,

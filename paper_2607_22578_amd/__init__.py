@@ -771,6 +771,9 @@ def merge_retrieval(keys, q_req, corpus, k: int, scale=None, workflow_offsets=No
 
 
 # ---------------------------------------------------------------- row tables
+#
+# As everything here these work on memory: no result has an autograd history.  A program
+# that trains calls embed and embed_grad from an autograd function of its own.
 
 class _Here:
     """The context of a call on the current device and stream."""
@@ -913,7 +916,8 @@ def embed(table: RowTable, ids, scale: float = 1.0, pad_id: int = -1, out_dtype=
     """Embedding lookup with scaling: scale * table[ids] for ids of any shape (int32 or
     int64), as ids.shape + [dim] in out_dtype (default: the table's type, bfloat16 for
     quantised tables).  Ids outside the table and pad_id give rows of zeros.  `out`:
-    a contiguous tensor for the result."""
+    a contiguous tensor for the result.  The result is not differentiable by itself;
+    embed_grad is its gradient."""
     torch = _torch
     device = table.device
     is64, n = _ids(ids, device)

@@ -10,7 +10,8 @@
 // Bound by the scores' bytes.  256 x 131,072 bf16, 1,000 tokens seen and 25 biases on
 // average, a mask per row (140 MB): 39 us, 3.6 TB/s (35 without lists).  (Counts in two words per column of a
 // 4,096-column tile took 53 to 70 us, with the chain of list, marks and scores paid
-// for each tile.)
+// for each tile.)  Each range reads all of its row's entries: 1 x 131,072 fp32 with 1,000, 10,000 and
+// 100,000 of them 11, 18 and 105 us; 256 rows with 20,000 each, taken in halves too, 1,470 us.
 #include "rows.h"
 
 namespace hs {
